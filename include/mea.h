@@ -206,6 +206,87 @@ mea_status mea_attention_bwd_noalloc(const mea_problem* p, const void* q, const 
                                      const void* d_o, const float* lse, void* dq, void* dk,
                                      void* dv, hipStream_t stream);
 
+/* ---- Attention with modified scores --------------------------------------
+ * With x_ij = scale * q_i . k_j, a position pos_i = q_pos[b] + i of query i
+ * (key j is at position j), and the distance j - pos_i:
+ *   y_ij = softcap * tanh(x_ij / softcap)              (softcap > 0; else x_ij)
+ *   s_ij = y_ij - slopes[h] * |pos_i - j| + table[bucket(j - pos_i), h]
+ *   o_i = sum_j softmax_j(s_ij) v_j, over the visible keys:
+ *   j < kv_len[b]; causal: j <= pos_i or j < prefix_len[b]; with documents:
+ *   q_doc[b, i] = k_doc[b, j], and not negative.
+ * A query with no visible key gets o = 0, lse = -inf and zero gradients; the
+ * values of keys j >= kv_len[b] and of tokens whose document is negative are
+ * never used, whatever they hold (NaN included).  Query head h reads key head
+ * h / (heads / kv_heads), and k, v, dk, dv are [B, kv_heads, n_k, d]: dk and dv
+ * are the sums over the heads that share a key head.
+ *
+ * Buckets: a side has n_edges buckets, bucket t for the distances from edges[t]
+ * to below edges[t + 1], the last for all from edges[n_edges - 1] on.  One-sided
+ * (two_sided = 0): the distance is max(pos_i - j, 0).  Two-sided: |j - pos_i|,
+ * and keys ahead (j > pos_i) take buckets n_edges .. 2 n_edges - 1.
+ *
+ * The mea_problem's own mask, padding, strides, dtype and scale hold as before
+ * (strides of k, v, dk and dv are over kv_heads); out_f32 must be 0 and d_v must
+ * be d.  Everything said above about pointers, streams, workspaces, errors and
+ * ownership holds here too. */
+#define MEA_MAX_SIDE_BUCKETS 64 /* n_edges */
+#define MEA_MAX_BIAS_SPAN 512   /* edges[n_edges - 1] */
+typedef struct {
+  int64_t kv_heads;          /* a divisor of heads; 0: heads */
+  float softcap;             /* > 0 and finite, or 0: none */
+  int32_t table_dtype;       /* mea_dtype of table */
+  const float* slopes;       /* DEVICE float32 [H], or NULL */
+  const void* table;         /* DEVICE [buckets, H], or NULL */
+  const int32_t* edges;      /* HOST [n_edges], from 0, not falling (read during the call only) */
+  int32_t n_edges;           /* 2 .. MEA_MAX_SIDE_BUCKETS; the last edge 1 .. MEA_MAX_BIAS_SPAN */
+  int32_t two_sided;         /* 0 or 1 */
+  const int32_t* q_doc;      /* DEVICE int32 [B, n_q], contiguous; NULL with k_doc: no documents */
+  const int32_t* k_doc;      /* DEVICE int32 [B, n_k] */
+  const int32_t* prefix_len; /* DEVICE int32 [B], with causal only; or NULL */
+  const int32_t* q_pos;      /* DEVICE int32 [B], negative values read as 0; or NULL: 0 */
+} mea_score;
+
+/* Bytes of device workspace of the two calls below (partial sums where the keys
+ * are split, ranges of document ids, per-row values of the backward, and the bias
+ * gradient's partial sums).  0 is possible for the forward only. */
+mea_status mea_scored_attention_fwd_workspace_size(const mea_problem* p, const mea_score* s, size_t* bytes);
+mea_status mea_scored_attention_bwd_workspace_size(const mea_problem* p, const mea_score* s, size_t* bytes);
+
+/* Forward; lse and o_lo as in mea_attention_fwd. */
+mea_status mea_scored_attention_fwd(const mea_problem* p, const mea_score* s, const void* q, const void* k,
+                                    const void* v, void* o, float* lse, void* o_lo, void* workspace,
+                                    size_t workspace_bytes, hipStream_t stream);
+
+/* Backward; o, o_lo, d_o, lse, dq, dk and dv as in mea_attention_bwd.  d_table
+ * ([buckets, H] in table_dtype, 4-byte aligned, or NULL) gets the bias's gradient
+ *   sum over batches and pairs of the bucket of w_ij (do_i . v_j - D_i)
+ * and needs dq.  The same sums in the same order on every call. */
+mea_status mea_scored_attention_bwd(const mea_problem* p, const mea_score* s, const void* q, const void* k,
+                                    const void* v, const void* o, const void* o_lo, const void* d_o, const float* lse,
+                                    void* dq, void* dk, void* dv, void* d_table, void* workspace, size_t workspace_bytes,
+                                    hipStream_t stream);
+
+/* ---- Attention of a batch that shares a prefix ----------------------------
+ * Every query of every sequence sees all n_p keys of the prefix, and its
+ * sequence's own keys as the mea_problem says (n_k, kv_len, causal with q_pos;
+ * positions count the own keys):
+ *   o = softmax over both sets of keys of scale * q . k, times their values.
+ * The prefix is read once for all the queries of a key head; the two sets'
+ * summaries (Section 4) are combined at the end.  A mea_problem's strides are
+ * of q, the own k and v, and o.  lse may be NULL.  n_p >= 1; kv_len[b] may be 0. */
+typedef struct {
+  int64_t kv_heads;         /* a divisor of heads; 0: heads */
+  int64_t n_p;              /* keys of the prefix */
+  const void* k;            /* DEVICE [kv_heads, n_p, d], 16-byte aligned */
+  const void* v;
+  mea_tensor_strides k_strides, v_strides; /* head and row (batch is not read); row 0: contiguous */
+  const int32_t* q_pos;     /* DEVICE int32 [B], or NULL: 0 */
+} mea_shared_prefix;
+mea_status mea_prefix_attention_fwd_workspace_size(const mea_problem* p, const mea_shared_prefix* x, size_t* bytes);
+mea_status mea_prefix_attention_fwd(const mea_problem* p, const mea_shared_prefix* x, const void* q, const void* k,
+                                    const void* v, void* o, float* lse, void* workspace, size_t workspace_bytes,
+                                    hipStream_t stream);
+
 /* Static description of a status code (never NULL). */
 const char* mea_status_string(mea_status s);
 

@@ -8,9 +8,13 @@ is the thin Python binding.
 """
 from .attention import (MemoryEfficientAttention, PackedQKVAttention, attention, attention_bwd,
                         attention_fwd, attention_packed, bwd_workspace_bytes, fwd_workspace_bytes)
+from .scored import (ScoredAttention, attention_scored, attention_scored_bwd, attention_scored_fwd,
+                     attention_shared_prefix, bucket_edges)
 from .nn import MultiheadAttention, TransformerBlock, TransformerLM
 
 __all__ = ["attention", "attention_fwd", "attention_bwd", "attention_packed", "MemoryEfficientAttention",
            "PackedQKVAttention",
+           "attention_scored", "attention_scored_fwd", "attention_scored_bwd", "ScoredAttention",
+           "attention_shared_prefix", "bucket_edges",
            "fwd_workspace_bytes", "bwd_workspace_bytes", "MultiheadAttention", "TransformerBlock",
            "TransformerLM"]

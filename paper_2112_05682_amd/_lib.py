@@ -35,8 +35,17 @@ EXPORTS = (
     "mea_attention_fwd",
     "mea_attention_bwd",
     "mea_attention_bwd_noalloc",
+    "mea_scored_attention_fwd_workspace_size",
+    "mea_scored_attention_bwd_workspace_size",
+    "mea_scored_attention_fwd",
+    "mea_scored_attention_bwd",
+    "mea_prefix_attention_fwd_workspace_size",
+    "mea_prefix_attention_fwd",
     "mea_status_string",
 )
+
+# MEA_MAX_SIDE_BUCKETS and MEA_MAX_BIAS_SPAN.
+MAX_SIDE_BUCKETS, MAX_BIAS_SPAN = 64, 512
 
 
 class MeaTensorStrides(ctypes.Structure):
@@ -70,6 +79,39 @@ class MeaProblem(ctypes.Structure):
     ]
 
 
+class MeaScore(ctypes.Structure):
+    """Mirror of ``mea_score``."""
+
+    _fields_ = [
+        ("kv_heads", ctypes.c_int64),
+        ("softcap", ctypes.c_float),
+        ("table_dtype", ctypes.c_int32),
+        ("slopes", ctypes.c_void_p),
+        ("table", ctypes.c_void_p),
+        ("edges", ctypes.POINTER(ctypes.c_int32)),
+        ("n_edges", ctypes.c_int32),
+        ("two_sided", ctypes.c_int32),
+        ("q_doc", ctypes.c_void_p),
+        ("k_doc", ctypes.c_void_p),
+        ("prefix_len", ctypes.c_void_p),
+        ("q_pos", ctypes.c_void_p),
+    ]
+
+
+class MeaSharedPrefix(ctypes.Structure):
+    """Mirror of ``mea_shared_prefix``."""
+
+    _fields_ = [
+        ("kv_heads", ctypes.c_int64),
+        ("n_p", ctypes.c_int64),
+        ("k", ctypes.c_void_p),
+        ("v", ctypes.c_void_p),
+        ("k_strides", MeaTensorStrides),
+        ("v_strides", MeaTensorStrides),
+        ("q_pos", ctypes.c_void_p),
+    ]
+
+
 class MeaError(RuntimeError):
     def __init__(self, name: str, status: int, message: str):
         super().__init__("%s failed: %s (status %d)" % (name, message, status))
@@ -96,8 +138,14 @@ def load(path: str = LIB_PATH):
     lib.mea_attention_fwd.argtypes = [prob, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.mea_attention_bwd.argtypes = [prob, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.mea_attention_bwd_noalloc.argtypes = [prob, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
-    for name in ("mea_attention_fwd_workspace_size", "mea_attention_bwd_workspace_size",
-                 "mea_attention_fwd", "mea_attention_bwd", "mea_attention_bwd_noalloc"):
+    score, prefix = ctypes.POINTER(MeaScore), ctypes.POINTER(MeaSharedPrefix)
+    lib.mea_scored_attention_fwd_workspace_size.argtypes = [prob, score, ctypes.POINTER(sz)]
+    lib.mea_scored_attention_bwd_workspace_size.argtypes = [prob, score, ctypes.POINTER(sz)]
+    lib.mea_scored_attention_fwd.argtypes = [prob, score, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.mea_scored_attention_bwd.argtypes = [prob, score, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.mea_prefix_attention_fwd_workspace_size.argtypes = [prob, prefix, ctypes.POINTER(sz)]
+    lib.mea_prefix_attention_fwd.argtypes = [prob, prefix, vp, vp, vp, vp, vp, vp, sz, vp]
+    for name in EXPORTS:
         getattr(lib, name).restype = ctypes.c_int
     lib.mea_status_string.argtypes = [ctypes.c_int]
     lib.mea_status_string.restype = ctypes.c_char_p
@@ -189,3 +237,37 @@ def bwd_noalloc(p: MeaProblem, q, k, v, o, o_lo, d_o, lse, dq, dk, dv, stream) -
     """The backward without a workspace argument (static device scratch)."""
     return load().mea_attention_bwd_noalloc(ctypes.byref(p), q, k, v, o, o_lo, d_o, lse, dq, dk,
                                             dv, stream)
+
+
+def _size(name: str, *structs) -> int:
+    out = ctypes.c_size_t(0)
+    check(name, getattr(load(), name)(*(ctypes.byref(x) for x in structs), ctypes.byref(out)))
+    return int(out.value)
+
+
+def scored_fwd_workspace_size(p: MeaProblem, s: MeaScore) -> int:
+    return _size("mea_scored_attention_fwd_workspace_size", p, s)
+
+
+def scored_bwd_workspace_size(p: MeaProblem, s: MeaScore) -> int:
+    return _size("mea_scored_attention_bwd_workspace_size", p, s)
+
+
+def prefix_fwd_workspace_size(p: MeaProblem, x: MeaSharedPrefix) -> int:
+    return _size("mea_prefix_attention_fwd_workspace_size", p, x)
+
+
+def scored_fwd(p: MeaProblem, s: MeaScore, q, k, v, o, lse, o_lo, workspace, workspace_bytes, stream) -> int:
+    return load().mea_scored_attention_fwd(ctypes.byref(p), ctypes.byref(s), q, k, v, o, lse, o_lo, workspace,
+                                           workspace_bytes, stream)
+
+
+def scored_bwd(p: MeaProblem, s: MeaScore, q, k, v, o, o_lo, d_o, lse, dq, dk, dv, d_table, workspace,
+               workspace_bytes, stream) -> int:
+    return load().mea_scored_attention_bwd(ctypes.byref(p), ctypes.byref(s), q, k, v, o, o_lo, d_o, lse, dq, dk, dv,
+                                           d_table, workspace, workspace_bytes, stream)
+
+
+def prefix_fwd(p: MeaProblem, x: MeaSharedPrefix, q, k, v, o, lse, workspace, workspace_bytes, stream) -> int:
+    return load().mea_prefix_attention_fwd(ctypes.byref(p), ctypes.byref(x), q, k, v, o, lse, workspace,
+                                           workspace_bytes, stream)

@@ -20,7 +20,9 @@ CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libmea.so")
 EXT = os.path.join(HERE, "_torch_ext.so")
-SOURCES = ["bwd_bf16.hip", "bwd_f16.hip", "bwd_f32.hip", "fwd.hip", "decode.hip", "api.hip", "bwd.hip"]
+SOURCES = ["bwd_bf16.hip", "bwd_f16.hip", "bwd_f32.hip", "fwd.hip", "decode.hip", "api.hip", "bwd.hip",
+           "scored_fwd_bf16.hip", "scored_fwd_f16.hip", "scored_fwd_f32.hip", "scored_bwd_bf16.hip", "scored_bwd_f16.hip",
+           "scored_bwd_f32.hip", "scored.hip", "scored_api.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

@@ -9,6 +9,7 @@
 #include <mutex>
 
 #include "../../include/mea.h"
+#include "checks.hpp"
 #include "kernels.hpp"
 
 // Per-row backward workspace of mea_attention_bwd_noalloc: one copy per GPU,
@@ -19,72 +20,12 @@ static __device__ __align__(256) unsigned char scratch[MEA_NOALLOC_SCRATCH_BYTES
 
 namespace {
 
+using namespace mea_host;
 using mea::BwdParams;
 using mea::FwdParams;
 
-constexpr int64_t kMaxSeq = (int64_t)1 << 31;  // n_q, n_k must stay below 2^31
-
-bool mul_ok(int64_t a, int64_t b, int64_t* out) {
-  if (a < 0 || b < 0) return false;
-  if (a != 0 && b > INT64_MAX / a) return false;
-  *out = a * b;
-  return true;
-}
-
-// Head dimension of v and o (d_v = 0 means d).
-int64_t dv_of(const mea_problem* p) { return p->d_v ? p->d_v : p->d; }
-
-// Shape, dtype and scale checks shared by every entry point.
-mea_status check_problem(const mea_problem* p) {
-  if (!p) return MEA_ERR_INVALID_ARG;
-  if (p->batch < 1 || p->heads < 1 || p->n_q < 1 || p->n_k < 1 || p->d < 1)
-    return MEA_ERR_INVALID_ARG;
-  if (p->n_q >= kMaxSeq || p->n_k >= kMaxSeq) return MEA_ERR_INVALID_ARG;
-  if (p->causal != 0 && p->causal != 1) return MEA_ERR_INVALID_ARG;
-  if (p->out_f32 != 0 && p->out_f32 != 1) return MEA_ERR_INVALID_ARG;
-  if (!(p->scale > 0.0f) || !isfinite(p->scale)) return MEA_ERR_INVALID_ARG;
-  if (p->kv_len && ((uintptr_t)p->kv_len & 3u)) return MEA_ERR_INVALID_ARG;
-  if (p->d_v < 0) return MEA_ERR_INVALID_ARG;
-  const int64_t dmax = p->d > dv_of(p) ? p->d : dv_of(p);
-  int64_t bh, nq_d, nk_d, tot;
-  if (!mul_ok(p->batch, p->heads, &bh) || bh >= kMaxSeq) return MEA_ERR_INVALID_ARG;
-  if (!mul_ok(p->n_q, dmax, &nq_d) || !mul_ok(p->n_k, dmax, &nk_d)) return MEA_ERR_INVALID_ARG;
-  if (!mul_ok(bh, nq_d, &tot) || !mul_ok(bh, nk_d, &tot)) return MEA_ERR_INVALID_ARG;
-  if (!mul_ok(bh, p->n_q * 4, &tot)) return MEA_ERR_INVALID_ARG;
-  if (p->d != 64 && p->d != 128) return MEA_ERR_UNSUPPORTED;
-  if (dv_of(p) != 64 && dv_of(p) != 128) return MEA_ERR_UNSUPPORTED;
-  if (p->dtype != MEA_F32 && p->dtype != MEA_F16 && p->dtype != MEA_BF16) return MEA_ERR_UNSUPPORTED;
-  return MEA_OK;
-}
-
-// Strides of a tensor of n rows of w features: given, or contiguous [B, H, n, w].
-mea::TensorStrides strides_of(const mea_problem* p, const mea_tensor_strides* given, int64_t n, int64_t w) {
-  if (given) return {given->batch, given->head, given->row};
-  return {p->heads * n * w, n * w, w};
-}
-
-// Validation of one tensor's strides (see mea.h); w = features per row.
-bool strides_ok(const mea_problem* p, const mea::TensorStrides& s, int64_t n, bool output, size_t elem,
-                int64_t w) {
-  const int64_t align = 16 / (int64_t)elem;
-  if (s.b < 0 || s.h < 0 || s.r < w || s.r >= ((int64_t)1 << 24)) return false;
-  if (output && (s.b == 0 || s.h == 0)) return false;
-  if (s.b % align || s.h % align || s.r % align) return false;
-  int64_t a, b, c, tot;
-  if (!mul_ok(p->batch - 1, s.b, &a) || !mul_ok(p->heads - 1, s.h, &b) || !mul_ok(n - 1, s.r, &c)) return false;
-  if (__builtin_add_overflow(a, b, &tot) || __builtin_add_overflow(tot, c, &tot) ||
-      __builtin_add_overflow(tot, w, &tot))
-    return false;
-  return true;
-}
-
-size_t elem_size(int32_t dtype) { return dtype == MEA_F32 ? 4 : 2; }
-
 // Whether o and do are float32 (float32 inputs, or 16-bit inputs with out_f32).
 bool out_is_f32(const mea_problem* p) { return p->dtype == MEA_F32 || p->out_f32 != 0; }
-
-bool aligned16(const void* ptr) { return ((uintptr_t)ptr & 15u) == 0; }
-bool dev_ptr_ok(const void* ptr) { return ptr != nullptr && aligned16(ptr); }
 
 struct FwdPlan {
   int bq, bk;
@@ -195,14 +136,6 @@ size_t bwd_workspace(const mea_problem* p, bool allow_do16) {
   const size_t rows = bwd_records(p, allow_do16) ? bwd_row_array_bytes(p, 16) : 2 * bwd_row_array_bytes(p, 4);
   return rows + (bwd_do16(p, allow_do16) ? bwd_do16_bytes(p) : 0) + 256;
 }
-
-float* align256(void* base, size_t off) {
-  uintptr_t a = (uintptr_t)base + off;
-  a = (a + 255u) & ~(uintptr_t)255u;
-  return reinterpret_cast<float*>(a);
-}
-
-constexpr float kLog2e = 1.4426950408889634f;
 
 // Device address of `scratch` on the current device, looked up once per
 // device (hipGetSymbolAddress with that device current) and cached.
@@ -319,12 +252,12 @@ mea_status mea_attention_fwd(const mea_problem* p, const void* q, const void* k,
     const mea_strides* st_ = p->strides;
     const size_t e = elem_size(p->dtype), eo = p->out_f32 && p->dtype != MEA_F32 ? 4 : e;
     const int64_t d = p->d, dv = dv_of(p);
-    fp.sq = strides_of(p, st_ ? &st_->q : nullptr, p->n_q, d);
-    fp.sk = strides_of(p, st_ ? &st_->k : nullptr, p->n_k, d);
-    fp.sv = strides_of(p, st_ ? &st_->v : nullptr, p->n_k, dv);
-    fp.so = strides_of(p, st_ ? &st_->o : nullptr, p->n_q, dv);
-    if (!strides_ok(p, fp.sq, p->n_q, false, e, d) || !strides_ok(p, fp.sk, p->n_k, false, e, d) ||
-        !strides_ok(p, fp.sv, p->n_k, false, e, dv) || !strides_ok(p, fp.so, p->n_q, true, eo, dv))
+    fp.sq = strides_of(st_ ? &st_->q : nullptr, p->heads, p->n_q, d);
+    fp.sk = strides_of(st_ ? &st_->k : nullptr, p->heads, p->n_k, d);
+    fp.sv = strides_of(st_ ? &st_->v : nullptr, p->heads, p->n_k, dv);
+    fp.so = strides_of(st_ ? &st_->o : nullptr, p->heads, p->n_q, dv);
+    if (!strides_ok(p->batch, p->heads, fp.sq, p->n_q, false, e, d) || !strides_ok(p->batch, p->heads, fp.sk, p->n_k, false, e, d) ||
+        !strides_ok(p->batch, p->heads, fp.sv, p->n_k, false, e, dv) || !strides_ok(p->batch, p->heads, fp.so, p->n_q, true, eo, dv))
       return MEA_ERR_INVALID_ARG;
   }
   if (pl.n_splits > 1) {
@@ -423,18 +356,18 @@ mea_status bwd_launch(const mea_problem* p, const void* q, const void* k, const 
     const mea_strides* st_ = p->strides;
     const size_t e = elem_size(p->dtype), eo = p->out_f32 && p->dtype != MEA_F32 ? 4 : e;
     const int64_t d = p->d, dvw = dv_of(p);
-    bp.sq = strides_of(p, st_ ? &st_->q : nullptr, p->n_q, d);
-    bp.sk = strides_of(p, st_ ? &st_->k : nullptr, p->n_k, d);
-    bp.sv = strides_of(p, st_ ? &st_->v : nullptr, p->n_k, dvw);
-    bp.so = strides_of(p, st_ ? &st_->o : nullptr, p->n_q, dvw);
-    bp.sdo = strides_of(p, st_ ? &st_->d_o : nullptr, p->n_q, dvw);
-    bp.sdq = strides_of(p, st_ ? &st_->dq : nullptr, p->n_q, d);
-    bp.sdk = strides_of(p, st_ ? &st_->dk : nullptr, p->n_k, d);
-    bp.sdv = strides_of(p, st_ ? &st_->dv : nullptr, p->n_k, dvw);
-    if (!strides_ok(p, bp.sq, p->n_q, false, e, d) || !strides_ok(p, bp.sk, p->n_k, false, e, d) ||
-        !strides_ok(p, bp.sv, p->n_k, false, e, dvw) || !strides_ok(p, bp.so, p->n_q, false, eo, dvw) ||
-        !strides_ok(p, bp.sdo, p->n_q, false, eo, dvw) || (dq && !strides_ok(p, bp.sdq, p->n_q, true, e, d)) ||
-        (dk && (!strides_ok(p, bp.sdk, p->n_k, true, e, d) || !strides_ok(p, bp.sdv, p->n_k, true, e, dvw))))
+    bp.sq = strides_of(st_ ? &st_->q : nullptr, p->heads, p->n_q, d);
+    bp.sk = strides_of(st_ ? &st_->k : nullptr, p->heads, p->n_k, d);
+    bp.sv = strides_of(st_ ? &st_->v : nullptr, p->heads, p->n_k, dvw);
+    bp.so = strides_of(st_ ? &st_->o : nullptr, p->heads, p->n_q, dvw);
+    bp.sdo = strides_of(st_ ? &st_->d_o : nullptr, p->heads, p->n_q, dvw);
+    bp.sdq = strides_of(st_ ? &st_->dq : nullptr, p->heads, p->n_q, d);
+    bp.sdk = strides_of(st_ ? &st_->dk : nullptr, p->heads, p->n_k, d);
+    bp.sdv = strides_of(st_ ? &st_->dv : nullptr, p->heads, p->n_k, dvw);
+    if (!strides_ok(p->batch, p->heads, bp.sq, p->n_q, false, e, d) || !strides_ok(p->batch, p->heads, bp.sk, p->n_k, false, e, d) ||
+        !strides_ok(p->batch, p->heads, bp.sv, p->n_k, false, e, dvw) || !strides_ok(p->batch, p->heads, bp.so, p->n_q, false, eo, dvw) ||
+        !strides_ok(p->batch, p->heads, bp.sdo, p->n_q, false, eo, dvw) || (dq && !strides_ok(p->batch, p->heads, bp.sdq, p->n_q, true, e, d)) ||
+        (dk && (!strides_ok(p->batch, p->heads, bp.sdk, p->n_k, true, e, d) || !strides_ok(p->batch, p->heads, bp.sdv, p->n_k, true, e, dvw))))
       return MEA_ERR_INVALID_ARG;
   }
   const hipError_t e = mea::launch_bwd(bp, p->dtype, (int)p->d, (int)dv_of(p), p->causal != 0,

@@ -1,0 +1,332 @@
+// Attention with modified scores: what the forward, the backward and the
+// shared-prefix kernels have in common.
+//
+//   x_ij = scale q_i . k_j
+//   y_ij = cap tanh(x_ij / cap)                       (x_ij without a cap)
+//   s_ij = y_ij - slope_h |pos_i - j| + table[bucket(j - pos_i), h]
+//   visible(i, j): j < lim_i and, with documents, q_doc_i = k_doc_j >= 0
+//   lim_i = valid keys of the batch; causal: and at most max(pos_i + 1, prefix)
+//   o_i = sum_j softmax_j(s_ij) v_j over the visible keys; none: o_i = 0, lse_i = -inf
+//
+// Every positional mask is one limit per query, so a tile of keys is plain (below
+// every limit of the workgroup), masked, or not visited.  Documents are told apart
+// by the smallest and largest id of every 32 tokens (doc_range_kernel): tiles whose
+// ranges do not meet are not visited, tiles of one document need no test.  The
+// learned bias is a function of the distance alone that is constant beyond its
+// span, so only the tiles within the span of the diagonal read it element by
+// element (from LDS); the others add one value.
+//
+// Scores are kept times log2 e from the cap or the bias on (weights are 2^s).
+#pragma once
+
+#include <type_traits>
+
+#include "device.hpp"
+#include "kernels.hpp"
+
+namespace mea {
+
+constexpr int kMaxSideBuckets = 64;  // MEA_MAX_SIDE_BUCKETS
+constexpr int kMaxBiasSpan = 512;    // MEA_MAX_BIAS_SPAN
+constexpr float kLog2eF = 1.4426950408889634f, kLn2F = 0.6931471805599453f;
+
+// What changes the scores (see mea_score in mea.h).
+struct ScoreArgs {
+  const float* slopes;   // [H] or null
+  const void* table;     // [buckets, H] or null
+  const int* q_doc;      // [B, n_q] or null
+  const int* k_doc;      // [B, n_k]
+  const int* q_pos;      // [B] or null
+  const int* prefix;     // [B] or null
+  const int* kv_len;     // [B] or null
+  const int2* q_range;   // smallest and largest id of every 32 queries, [B, ceil(n_q / 32)]
+  const int2* k_range;   // of every 32 keys
+  float cap2;            // cap * log2 e
+  float cap_in;          // scores to the argument of the cap's 2^x: 2 log2 e scale / cap
+  float cap_small;       // scores to the argument of tanh: scale / cap
+  int causal;
+  int table_dtype;       // mea_dtype
+  int heads;             // H
+  int n_edges, two_sided, span;
+  int edges[kMaxSideBuckets];  // smallest distance of each bucket of a side
+  int n_buckets() const { return n_edges * (two_sided ? 2 : 1); }
+};
+
+// Arguments of the stream kernel: rows (queries of the heads that share a key
+// head, of one batch or of all) against keys.
+struct StreamParams {
+  const void* q;
+  const void* k;
+  const void* v;
+  void* o;
+  float* lse;     // [B, H, n_q] or null
+  void* o_lo;     // contiguous [B, H, n_q, D] or null
+  float* part_o;  // summaries of the key ranges, [n_parts, B * H * n_q, D] and two of [n_parts, B * H * n_q]
+  float* part_m;
+  float* part_l;
+  int64_t n_q, n_k;
+  int64_t out_rows;    // B * H * n_q
+  int64_t group_rows;  // rows of a group: batches * n_q * fold
+  int fold;            // heads of a group, whose rows alternate: row r is head r % fold of query r / fold
+  int batches;         // batches of a group (1, or all of a shared prefix)
+  int n_b;             // batches over the groups (B, or 1)
+  int groups_per_kv;   // groups that share a key head: (H / H_kv) / fold
+  int heads_per_kv;    // H / H_kv
+  int n_groups, n_rtiles, n_splits;
+  int split0;          // first summary of this launch
+  int direct;          // 1: one range, o and lse are written; 0: summaries
+  int tile_order;
+  float scale_log2;
+  TensorStrides sq, sk, sv, so;
+  ScoreArgs s;
+};
+
+// Chunk swizzle of a row of D 16-bit features: physical 16-byte chunk x ^ swz(r).
+// Rows of 256 bytes (one LDS line) spread 16 consecutive rows over 16 chunks and 4
+// consecutive rows over the 4 groups of 4; rows of 128 bytes (two to a line) spread
+// 8 pairs of rows over 8 chunks and neighbouring pairs over the 2 groups of 4: row
+// reads and transposing reads of the same tile are both free of bank conflicts.
+template <int D>
+__device__ __forceinline__ int swz(int r) {
+  return D == 128 ? ((r & 3) << 2) | ((r >> 2) & 3) : (((r >> 1) & 1) << 2) | ((r >> 2) & 3);
+}
+template <typename T, int D>
+__device__ __forceinline__ Frag<T> row_frag(const unsigned char* tile, int r, int x) {
+  return *reinterpret_cast<const Frag<T>*>(tile + r * (2 * D) + ((x ^ swz<D>(r)) << 4));
+}
+template <typename T, int D>
+__device__ __forceinline__ Frag<T> col_frag(const unsigned char* tile, int row0, int col0, int lane) {
+  const int g = lane >> 4, i = lane & 15;
+  const int row = row0 + 8 * (g >> 1) + (i >> 2);
+  const int col = col0 + 16 * (g & 1) + 4 * (i & 3);
+  const int off = (col & 7) << 1;
+  const v4s_t lo = lds_read_tr16(tile + row * (2 * D) + (((col >> 3) ^ swz<D>(row)) << 4) + off);
+  const v4s_t hi = lds_read_tr16(tile + (row + 4) * (2 * D) + (((col >> 3) ^ swz<D>(row + 4)) << 4) + off);
+  typedef short v8s_t __attribute__((ext_vector_type(8)));
+  v8s_t r8;
+  r8[0] = lo[0]; r8[1] = lo[1]; r8[2] = lo[2]; r8[3] = lo[3];
+  r8[4] = hi[0]; r8[5] = hi[1]; r8[6] = hi[2]; r8[7] = hi[3];
+  return __builtin_bit_cast(Frag<T>, r8);
+}
+
+// A value of the bias table, times log2 e.
+__device__ __forceinline__ float table_value(const ScoreArgs& s, int bucket, int head) {
+  const int64_t at = (int64_t)bucket * s.heads + head;
+  float x;
+  if (s.table_dtype == 0) x = static_cast<const float*>(s.table)[at];
+  else if (s.table_dtype == 1) x = (float)static_cast<const _Float16*>(s.table)[at];
+  else x = (float)static_cast<const __bf16*>(s.table)[at];
+  return x * kLog2eF;
+}
+// Bucket of a side for a distance >= 0: the last one that starts at most there.
+__device__ __forceinline__ int side_bucket(const ScoreArgs& s, int distance) {
+  int n = 0;
+  for (int e = 0; e < s.n_edges; ++e) n += s.edges[e] <= distance;
+  return n - 1;
+}
+// The bias by place: place x stands for j - pos = x - span (clamped to +-span,
+// or to [-span, 0] where keys ahead count as distance 0).
+__host__ __device__ __forceinline__ int bias_places(const ScoreArgs& s) {
+  return s.table ? (s.two_sided ? 2 * s.span + 1 : s.span + 1) : 0;
+}
+__device__ __forceinline__ int place_bucket(const ScoreArgs& s, int x) {
+  const int d = x - s.span;
+  return side_bucket(s, d < 0 ? -d : d) + (d > 0 ? s.n_edges : 0);
+}
+// LDS bytes of the bias for fold heads: the values by place, or (several heads)
+// each place's bucket and the heads' buckets.
+__host__ __device__ __forceinline__ int bias_lds_bytes(const ScoreArgs& s, int fold) {
+  const int n = bias_places(s);
+  if (!n) return 0;
+  if (fold == 1) return (4 * n + 15) / 16 * 16;
+  return (n + 15) / 16 * 16 + (4 * fold * s.n_edges * (s.two_sided ? 2 : 1) + 15) / 16 * 16;
+}
+__device__ __forceinline__ void fill_bias(const ScoreArgs& s, unsigned char* lds, int fold, int head0, int tid, int nt) {
+  const int n = bias_places(s);
+  if (fold == 1) {
+    for (int x = tid; x < n; x += nt) reinterpret_cast<float*>(lds)[x] = table_value(s, place_bucket(s, x), head0);
+    return;
+  }
+  for (int x = tid; x < n; x += nt) lds[x] = (unsigned char)place_bucket(s, x);
+  const int nb = s.n_edges * (s.two_sided ? 2 : 1);
+  float* tab = reinterpret_cast<float*>(lds + (n + 15) / 16 * 16);
+  for (int e = tid; e < fold * nb; e += nt) tab[e] = table_value(s, e % nb, head0 + e / nb);
+}
+// The bias at a place for head g of the fold.
+__device__ __forceinline__ float bias_at(const ScoreArgs& s, const unsigned char* lds, int fold, int g, int x) {
+  if (fold == 1) return reinterpret_cast<const float*>(lds)[x];
+  const int n = bias_places(s);
+  return reinterpret_cast<const float*>(lds + (n + 15) / 16 * 16)[g * s.n_edges * (s.two_sided ? 2 : 1) + lds[x]];
+}
+
+// tanh of scale x / cap.  With e = 2^(2 log2 e scale x / cap) it is 1 - 2 / (1 + e),
+// off by a few 2^-24 in all; float32 scores, whose small values are exact to 2^-24 of
+// themselves, take the series of small arguments instead.
+template <typename T>
+__device__ __forceinline__ float cap_tanh(const ScoreArgs& s, float x) {
+  const float e = fast_exp2(x * s.cap_in);
+  float t = fmaf(-2.0f, __builtin_amdgcn_rcpf(1.0f + e), 1.0f);
+  if constexpr (sizeof(T) == 4) {
+    // y - y^3/3 + 2 y^5/15 - 17 y^7/315 + 62 y^9/2835 - 1382 y^11/155925: below 0.35
+    // the next term is under 2^-26 of y.
+    const float y = x * s.cap_small, z = y * y;
+    const float a = y * fmaf(z, fmaf(z, fmaf(z, fmaf(z, fmaf(z, -8.863235e-3f, 2.1869488e-2f), -5.3968254e-2f),
+                                             1.3333333e-1f), -3.3333333e-1f), 1.0f);
+    t = fabsf(y) < 0.35f ? a : t;
+  }
+  return t;
+}
+
+// Keys visible to a query by position: [0, lim).
+__device__ __forceinline__ int64_t key_limit(const ScoreArgs& s, int b, int64_t n_kv, int64_t pos) {
+  if (!s.causal) return n_kv;
+  int64_t lim = pos + 1;
+  if (s.prefix && s.prefix[b] > lim) lim = s.prefix[b];
+  return lim < n_kv ? lim : n_kv;
+}
+__device__ __forceinline__ int64_t first_pos(const ScoreArgs& s, int b) {
+  const int p = s.q_pos ? s.q_pos[b] : 0;
+  return p > 0 ? p : 0;
+}
+__device__ __forceinline__ int64_t batch_keys(const ScoreArgs& s, int b, int64_t n_k) {
+  if (!s.kv_len) return n_k;
+  const int64_t l = s.kv_len[b];
+  return l < 0 ? 0 : (l > n_k ? n_k : l);
+}
+// A difference of positions as an int that still orders and clamps right.
+__device__ __forceinline__ int rel(int64_t x) {
+  constexpr int64_t kFar = (int64_t)1 << 30;
+  return (int)(x < -kFar ? -kFar : (x > kFar ? kFar : x));
+}
+
+// Smallest and largest id of a wave's 64 lanes.
+__device__ __forceinline__ int2 wave_range(int lo, int hi) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) {
+    const int a = __shfl_xor(lo, o), b = __shfl_xor(hi, o);
+    lo = a < lo ? a : lo;
+    hi = b > hi ? b : hi;
+  }
+  return make_int2(__builtin_amdgcn_readfirstlane(lo), __builtin_amdgcn_readfirstlane(hi));
+}
+
+// Smallest and largest id of a workgroup's tokens and (z) whether one of them has
+// none; id < 0: none.  Every thread of the 4 waves calls it.
+__device__ __forceinline__ int4 workgroup_ids(int id, int wave, int lane, int4* lds) {
+  const int2 w = wave_range(id < 0 ? 0x7fffffff : id, id);
+  const int none = __builtin_amdgcn_ballot_w64(id < 0) != 0;
+  if (lane == 0) lds[wave] = make_int4(w.x, w.y, none, 0);
+  __syncthreads();
+  int4 a = lds[0];
+#pragma unroll
+  for (int y = 1; y < 4; ++y) {
+    const int4 o = lds[y];
+    a.x = o.x < a.x ? o.x : a.x;
+    a.y = o.y > a.y ? o.y : a.y;
+    a.z |= o.z;
+  }
+  return make_int4(__builtin_amdgcn_readfirstlane(a.x), __builtin_amdgcn_readfirstlane(a.y),
+                   __builtin_amdgcn_readfirstlane(a.z), 0);
+}
+
+// A fragment without the elements whose bits are set, whatever they hold.
+template <typename T>
+__device__ __forceinline__ Frag<T> without(Frag<T> a, uint32_t bits) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+    if (bits >> e & 1) {
+      if constexpr (sizeof(T) == 4) a.p[0][e] = a.p[1][e] = a.p[2][e] = (__bf16)0.0f;
+      else a[e] = (T)0.0f;
+    }
+  return a;
+}
+
+// Tiles of one side that may meet the ids [lo, hi]: 64 tiles at a time, a bit each.
+// Ranges are of 32 tokens, UNITS of them a tile.
+template <int UNITS>
+struct DocTiles {
+  const int2* range;  // of this batch, or null: every tile is visited
+  int n_units, lo, hi, base;
+  uint64_t bits;
+  __device__ __forceinline__ DocTiles(const int2* r, int n, int l, int h_) : range(r), n_units(n), lo(l), hi(h_), base(-64), bits(0) {}
+  __device__ __forceinline__ int2 of_tile(int t) const {
+    int2 x = make_int2(0x7fffffff, -1);
+#pragma unroll
+    for (int u = 0; u < UNITS; ++u)
+      if (t * UNITS + u < n_units) {
+        const int2 y = range[t * UNITS + u];
+        x.x = y.x < x.x ? y.x : x.x;
+        x.y = y.y > x.y ? y.y : x.y;
+      }
+    return x;
+  }
+  // The first tile >= t and < end to visit, or end.  t never decreases.
+  __device__ __forceinline__ int next(int t, int end) {
+    if (!range) return t;
+    while (t < end) {
+      if (t >= base + 64 || base < 0) {
+        base = t;
+        const int mine = t + (int)(threadIdx.x & 63);
+        const int2 x = of_tile(mine);
+        bits = __builtin_amdgcn_ballot_w64(mine < end && x.x <= hi && x.y >= lo);
+      }
+      const uint64_t left = bits >> (t - base);
+      if (left) {
+        const int at = t + __builtin_ctzll(left);
+        return at < end ? at : end;
+      }
+      t = base + 64;
+    }
+    return end;
+  }
+  // Whether a tile holds the ids [lo, hi] only, all the same.
+  __device__ __forceinline__ bool uniform(int t) const {
+    if (!range) return true;
+    const int2 x = of_tile(t);
+    return lo == hi && x.x == lo && x.y == lo;
+  }
+};
+
+// Arguments of the backward kernels.
+struct ScoredBwdParams {
+  const void* q;
+  const void* k;
+  const void* v;
+  const void* o;
+  const void* o_lo;  // residual of a 16-bit o (contiguous [B, H, n_q, D]) or null
+  const void* d_o;
+  const float* lse;
+  void* dq;
+  void* dk;
+  void* dv;
+  // Per row, [B * H, n_q_pad], written by the preprocess: lse log2 e (inf for a row
+  // with no visible key and for padding, whose weights are then 0) and -D_i.
+  float* lse2;
+  float* neg_d;
+  float* table_part;  // dS sums by bucket of each dQ workgroup, [n_wgs, buckets], or null
+  void* d_table;      // [buckets, H], the table's type
+  int64_t n_q, n_k, n_q_pad;
+  int n_b, heads_kv, heads_per_kv;
+  int n_ktiles, n_qtiles, tile_order;
+  float scale, scale_log2;
+  TensorStrides sq, sk, sv, so, sdo, sdq, sdk, sdv;
+  ScoreArgs s;
+};
+
+hipError_t launch_scored_table(const ScoredBwdParams& p, hipStream_t stream);
+hipError_t launch_doc_ranges(const int* ids, int64_t n, int64_t batches, int2* out, hipStream_t stream);
+
+// Rows per workgroup: 32 for each of 4 waves, or 2 or 1 (the other waves take
+// shares of the keys).
+template <typename T> hipError_t launch_stream(const StreamParams& p, int d, int row_waves, hipStream_t stream);
+template <typename T>
+hipError_t launch_scored_combine(const StreamParams& p, int d, int n_parts, hipStream_t stream);
+template <typename T> hipError_t launch_scored_bwd(const ScoredBwdParams& p, int d, hipStream_t stream);
+// Rows of a dQ workgroup (the plan sizes table_part by it), and the row padding.
+constexpr int kScoredDqRows = 128, kScoredRowPad = 64;
+// Keys of a staged tile.
+__host__ __device__ constexpr int stream_tile(bool is16, int row_waves) {
+  return is16 ? (row_waves == 1 ? 128 : 64) : (row_waves == 4 ? 32 : 64);
+}
+
+}  // namespace mea

@@ -1,0 +1,445 @@
+// Entry points of attention with modified scores and of attention over a shared
+// prefix: argument checks, work planning and dispatch.  Nothing here allocates
+// device memory or synchronises.
+#include <string.h>
+
+#include "checks.hpp"
+#include "scored.hpp"
+
+namespace {
+
+using namespace mea_host;
+using mea::ScoreArgs;
+using mea::ScoredBwdParams;
+using mea::StreamParams;
+
+static_assert(mea::kMaxSideBuckets == MEA_MAX_SIDE_BUCKETS && mea::kMaxBiasSpan == MEA_MAX_BIAS_SPAN, "limits");
+
+bool aligned4(const void* p) { return ((uintptr_t)p & 3u) == 0; }
+int64_t kv_heads_of(const mea_problem* p, int64_t given) { return given ? given : p->heads; }
+
+mea_status check_base(const mea_problem* p, int64_t kv_heads) {
+  const mea_status st = check_problem(p);
+  if (st != MEA_OK) return st;
+  if (kv_heads < 0 || (kv_heads && p->heads % kv_heads)) return MEA_ERR_INVALID_ARG;
+  if (p->out_f32 && p->dtype != MEA_F32) return MEA_ERR_UNSUPPORTED;
+  if (dv_of(p) != p->d) return MEA_ERR_UNSUPPORTED;
+  return MEA_OK;
+}
+
+mea_status check_score(const mea_problem* p, const mea_score* s) {
+  if (!s) return MEA_ERR_INVALID_ARG;
+  const mea_status st = check_base(p, s->kv_heads);
+  if (st != MEA_OK) return st;
+  if (!(s->softcap >= 0.0f) || !isfinite(s->softcap)) return MEA_ERR_INVALID_ARG;
+  if (s->softcap > 0.0f && !(s->softcap * kLog2e > 0.0f && isfinite(s->softcap * kLog2e) && isfinite(2.0f * kLog2e * p->scale / s->softcap)))
+    return MEA_ERR_INVALID_ARG;
+  if (!aligned4(s->slopes) || !aligned4(s->q_doc) || !aligned4(s->k_doc) || !aligned4(s->prefix_len) || !aligned4(s->q_pos) ||
+      !aligned4(s->table))
+    return MEA_ERR_INVALID_ARG;
+  if ((s->q_doc == nullptr) != (s->k_doc == nullptr)) return MEA_ERR_INVALID_ARG;
+  if (s->prefix_len && !p->causal) return MEA_ERR_INVALID_ARG;
+  if (s->table) {
+    if (s->table_dtype != MEA_F32 && s->table_dtype != MEA_F16 && s->table_dtype != MEA_BF16) return MEA_ERR_UNSUPPORTED;
+    if (s->two_sided != 0 && s->two_sided != 1) return MEA_ERR_INVALID_ARG;
+    if (!s->edges || s->n_edges < 2 || s->edges[0] != 0) return MEA_ERR_INVALID_ARG;
+    if (s->n_edges > MEA_MAX_SIDE_BUCKETS) return MEA_ERR_UNSUPPORTED;
+    for (int i = 1; i < s->n_edges; ++i)
+      if (s->edges[i] < s->edges[i - 1]) return MEA_ERR_INVALID_ARG;
+    if (s->edges[s->n_edges - 1] < 1) return MEA_ERR_INVALID_ARG;
+    if (s->edges[s->n_edges - 1] > MEA_MAX_BIAS_SPAN) return MEA_ERR_UNSUPPORTED;
+  }
+  return MEA_OK;
+}
+
+ScoreArgs score_args(const mea_problem* p, const mea_score* s) {
+  ScoreArgs a = {};
+  a.kv_len = p->kv_len;
+  a.causal = p->causal;
+  a.heads = (int)p->heads;
+  if (!s) return a;
+  a.slopes = s->slopes;
+  a.q_doc = s->q_doc;
+  a.k_doc = s->k_doc;
+  a.q_pos = s->q_pos;
+  a.prefix = s->prefix_len;
+  if (s->softcap > 0.0f) {
+    a.cap2 = s->softcap * kLog2e;
+    a.cap_in = 2.0f * kLog2e * p->scale / s->softcap;
+    a.cap_small = p->scale / s->softcap;
+  }
+  if (s->table) {
+    a.table = s->table;
+    a.table_dtype = s->table_dtype;
+    a.n_edges = s->n_edges;
+    a.two_sided = s->two_sided;
+    a.span = s->edges[s->n_edges - 1];
+    memcpy(a.edges, s->edges, sizeof(int) * (size_t)s->n_edges);
+  }
+  return a;
+}
+
+size_t round256(size_t b) { return (b + 255) / 256 * 256; }
+size_t range_bytes(int64_t batch, int64_t n) { return round256((size_t)batch * (size_t)((n + 31) / 32) * sizeof(int2)); }
+
+// How rows meet keys in the stream kernel.
+struct StreamPlan {
+  int row_waves;
+  int64_t fold, groups, rows, rtiles, splits;  // rows of a group
+};
+
+// Fold: with few queries the heads that share a key head are rows of the same
+// tile, so that the keys are read once for all of them; with many, each head has
+// tiles of its own (the keys are then found in L2).  Row waves: as few as hold
+// the rows, and on small grids fewer still, so that the waves without rows of
+// their own take shares of the keys instead.  Splits: enough key ranges for about
+// one workgroup for each place on the chip, of at least two tiles each.
+StreamPlan plan_stream(const mea_problem* p, const ScoreArgs& s, int64_t kv_heads, bool shared, int64_t n_keys) {
+  StreamPlan pl;
+  const bool is16 = p->dtype != MEA_F32;
+  const int64_t G = p->heads / kv_heads;
+  const int least = is16 ? 1 : 2;
+  pl.fold = shared || G * p->n_q <= 64 ? G : 1;
+  // The biases of the folded heads have to fit beside the stages.
+  if (pl.fold > 1 && mea::bias_lds_bytes(s, (int)pl.fold) > 24 * 1024) pl.fold = 1;
+  pl.rows = (shared ? p->batch : 1) * p->n_q * pl.fold;
+  pl.groups = (p->heads / pl.fold) * (shared ? 1 : p->batch);
+  const int64_t tiles128 = pl.groups * ((pl.rows + 127) / 128);
+  int rw = tiles128 <= 128 ? 1 : (tiles128 <= 256 ? 2 : 4);
+  if (pl.rows <= 32) rw = 1;
+  else if (pl.rows <= 64 && rw > 2) rw = 2;
+  if (!is16) rw = pl.rows <= 64 || tiles128 <= 32 ? 2 : 4;
+  if (rw < least) rw = least;
+  pl.row_waves = rw;
+  pl.rtiles = (pl.rows + 32 * rw - 1) / (32 * rw);
+  const int64_t wgs = pl.groups * pl.rtiles;
+  const int64_t key_tiles = (n_keys + mea::stream_tile(is16, rw) - 1) / mea::stream_tile(is16, rw);
+  int64_t places = 256 * (is16 ? (rw == 1 ? (p->d == 64 ? 2 : 1) : 2) : 1);
+  int64_t splits = wgs * 2 > places ? 1 : places / wgs;
+  if (splits > key_tiles / 2) splits = key_tiles / 2;
+  if (splits > 64) splits = 64;
+  pl.splits = splits < 1 ? 1 : splits;
+  return pl;
+}
+
+size_t part_bytes(const mea_problem* p, int64_t parts) {
+  const size_t rows = (size_t)parts * (size_t)p->batch * (size_t)p->heads * (size_t)p->n_q;
+  return round256(rows * (size_t)p->d * 4) + 2 * round256(rows * 4);
+}
+void carve_parts(StreamParams* q, const mea_problem* p, int64_t parts, float* at) {
+  const size_t rows = (size_t)parts * (size_t)q->out_rows;
+  q->part_o = at;
+  q->part_m = at + round256(rows * (size_t)p->d * 4) / 4;
+  q->part_l = q->part_m + round256(rows * 4) / 4;
+}
+
+struct FwdWork {
+  StreamPlan pl;
+  size_t ranges, total;
+};
+FwdWork plan_scored_fwd(const mea_problem* p, const mea_score* s) {
+  FwdWork w;
+  w.pl = plan_stream(p, score_args(p, s), kv_heads_of(p, s->kv_heads), false, p->n_k);
+  w.ranges = s->q_doc ? range_bytes(p->batch, p->n_k) : 0;
+  w.total = w.ranges + (w.pl.splits > 1 ? part_bytes(p, w.pl.splits) : 0);
+  if (w.total) w.total += 256;
+  return w;
+}
+
+StreamParams stream_params(const mea_problem* p, const ScoreArgs& s, int64_t kv_heads, const StreamPlan& pl) {
+  StreamParams q = {};
+  q.s = s;
+  q.n_q = p->n_q;
+  q.n_k = p->n_k;
+  q.out_rows = p->batch * p->heads * p->n_q;
+  q.group_rows = pl.rows;
+  q.fold = (int)pl.fold;
+  q.batches = 1;
+  q.n_b = (int)p->batch;
+  q.heads_per_kv = (int)(p->heads / kv_heads);
+  q.groups_per_kv = q.heads_per_kv / q.fold;
+  q.n_groups = (int)pl.groups;
+  q.n_splits = (int)pl.splits;
+  q.scale_log2 = p->scale * kLog2e;
+  return q;
+}
+
+hipError_t run_stream(const StreamParams& q, const mea_problem* p, int row_waves, hipStream_t stream) {
+  const int d = (int)p->d;
+  switch (p->dtype) {
+    case MEA_F32: return mea::launch_stream<float>(q, d, row_waves, stream);
+    case MEA_F16: return mea::launch_stream<_Float16>(q, d, row_waves, stream);
+    default: return mea::launch_stream<__bf16>(q, d, row_waves, stream);
+  }
+}
+hipError_t run_combine(const StreamParams& q, const mea_problem* p, int parts, hipStream_t stream) {
+  const int d = (int)p->d;
+  switch (p->dtype) {
+    case MEA_F32: return mea::launch_scored_combine<float>(q, d, parts, stream);
+    case MEA_F16: return mea::launch_scored_combine<_Float16>(q, d, parts, stream);
+    default: return mea::launch_scored_combine<__bf16>(q, d, parts, stream);
+  }
+}
+
+mea_status status_of(hipError_t e) { return e == hipSuccess ? MEA_OK : MEA_ERR_HIP; }
+
+// Grids and thread counts that one launch has to hold.
+bool fits_launch(int64_t wgs) { return wgs < ((int64_t)1 << 31) / 256; }
+
+struct BwdWork {
+  int64_t n_q_pad, n_qtiles;
+  size_t rows, ranges_q, ranges_k, table, total;
+};
+BwdWork plan_scored_bwd(const mea_problem* p, const mea_score* s) {
+  BwdWork w = {};
+  w.n_q_pad = (p->n_q + mea::kScoredRowPad - 1) / mea::kScoredRowPad * mea::kScoredRowPad;
+  w.n_qtiles = (p->n_q + mea::kScoredDqRows - 1) / mea::kScoredDqRows;
+  w.rows = round256((size_t)p->batch * (size_t)p->heads * (size_t)w.n_q_pad * 4);
+  if (s->q_doc) {
+    w.ranges_q = range_bytes(p->batch, p->n_q);
+    w.ranges_k = range_bytes(p->batch, p->n_k);
+  }
+  if (s->table)
+    w.table = round256((size_t)p->batch * (size_t)p->heads * (size_t)w.n_qtiles * (size_t)s->n_edges * (s->two_sided ? 2 : 1) * 4);
+  w.total = 2 * w.rows + w.ranges_q + w.ranges_k + w.table + 256;
+  return w;
+}
+
+mea_status check_prefix(const mea_problem* p, const mea_shared_prefix* x) {
+  if (!x) return MEA_ERR_INVALID_ARG;
+  const mea_status st = check_base(p, x->kv_heads);
+  if (st != MEA_OK) return st;
+  if (x->n_p < 1 || x->n_p >= kMaxSeq || !aligned4(x->q_pos)) return MEA_ERR_INVALID_ARG;
+  int64_t rows;
+  if (!mul_ok(p->batch * p->heads, p->n_q, &rows) || rows >= kMaxSeq) return MEA_ERR_INVALID_ARG;
+  return MEA_OK;
+}
+struct PrefixWork {
+  StreamPlan shared, own;
+  size_t total;
+};
+PrefixWork plan_prefix(const mea_problem* p, const mea_shared_prefix* x) {
+  PrefixWork w;
+  const ScoreArgs none = {};
+  const int64_t kv = kv_heads_of(p, x->kv_heads);
+  w.shared = plan_stream(p, none, kv, true, x->n_p);
+  w.own = plan_stream(p, none, kv, false, p->n_k);
+  w.total = part_bytes(p, w.shared.splits + w.own.splits) + 256;
+  return w;
+}
+
+}  // namespace
+
+extern "C" {
+
+mea_status mea_scored_attention_fwd_workspace_size(const mea_problem* p, const mea_score* s, size_t* bytes) {
+  const mea_status st = check_score(p, s);
+  if (st != MEA_OK) return st;
+  if (!bytes) return MEA_ERR_INVALID_ARG;
+  *bytes = plan_scored_fwd(p, s).total;
+  return MEA_OK;
+}
+
+mea_status mea_scored_attention_bwd_workspace_size(const mea_problem* p, const mea_score* s, size_t* bytes) {
+  const mea_status st = check_score(p, s);
+  if (st != MEA_OK) return st;
+  if (!bytes) return MEA_ERR_INVALID_ARG;
+  *bytes = plan_scored_bwd(p, s).total;
+  return MEA_OK;
+}
+
+mea_status mea_scored_attention_fwd(const mea_problem* p, const mea_score* s, const void* q, const void* k, const void* v,
+                                    void* o, float* lse, void* o_lo, void* workspace, size_t workspace_bytes,
+                                    hipStream_t stream) {
+  const mea_status st = check_score(p, s);
+  if (st != MEA_OK) return st;
+  if (!dev_ptr_ok(q) || !dev_ptr_ok(k) || !dev_ptr_ok(v) || !dev_ptr_ok(o)) return MEA_ERR_INVALID_ARG;
+  if (lse && !aligned16(lse)) return MEA_ERR_INVALID_ARG;
+  if (o_lo && (!aligned16(o_lo) || p->dtype == MEA_F32)) return MEA_ERR_INVALID_ARG;
+  const int64_t kv = kv_heads_of(p, s->kv_heads);
+  const FwdWork w = plan_scored_fwd(p, s);
+  if (w.total && (!workspace || workspace_bytes < w.total)) return MEA_ERR_WORKSPACE;
+  StreamParams a = stream_params(p, score_args(p, s), kv, w.pl);
+  a.q = q;
+  a.k = k;
+  a.v = v;
+  a.o = o;
+  a.lse = lse;
+  a.o_lo = o_lo;
+  {
+    const mea_strides* t = p->strides;
+    const size_t e = elem_size(p->dtype);
+    a.sq = strides_of(t ? &t->q : nullptr, p->heads, p->n_q, p->d);
+    a.sk = strides_of(t ? &t->k : nullptr, kv, p->n_k, p->d);
+    a.sv = strides_of(t ? &t->v : nullptr, kv, p->n_k, p->d);
+    a.so = strides_of(t ? &t->o : nullptr, p->heads, p->n_q, p->d);
+    if (!strides_ok(p->batch, p->heads, a.sq, p->n_q, false, e, p->d) || !strides_ok(p->batch, kv, a.sk, p->n_k, false, e, p->d) ||
+        !strides_ok(p->batch, kv, a.sv, p->n_k, false, e, p->d) || !strides_ok(p->batch, p->heads, a.so, p->n_q, true, e, p->d))
+      return MEA_ERR_INVALID_ARG;
+  }
+  const int64_t grid = w.pl.rtiles * w.pl.groups * w.pl.splits;
+  if (!fits_launch(grid) || !fits_launch((a.out_rows * p->d / 4 + 255) / 256)) return MEA_ERR_INVALID_ARG;
+  if (p->causal)
+    a.tile_order = mea::causal_tile_order(p->batch * kv * p->n_k * 2 * p->d * (int64_t)elem_size(p->dtype), grid, true);
+  float* at = align256(workspace, 0);
+  if (s->q_doc) {
+    int2* r = reinterpret_cast<int2*>(at);
+    a.s.k_range = r;
+    const hipError_t e = mea::launch_doc_ranges(s->k_doc, p->n_k, p->batch, r, stream);
+    if (e != hipSuccess) return MEA_ERR_HIP;
+  }
+  a.direct = w.pl.splits == 1;
+  if (!a.direct) carve_parts(&a, p, w.pl.splits, at + w.ranges / 4);
+  const hipError_t e = run_stream(a, p, w.pl.row_waves, stream);
+  if (e != hipSuccess || a.direct) return status_of(e);
+  return status_of(run_combine(a, p, (int)w.pl.splits, stream));
+}
+
+mea_status mea_scored_attention_bwd(const mea_problem* p, const mea_score* s, const void* q, const void* k, const void* v,
+                                    const void* o, const void* o_lo, const void* d_o, const float* lse, void* dq, void* dk,
+                                    void* dv, void* d_table, void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  const mea_status st = check_score(p, s);
+  if (st != MEA_OK) return st;
+  if (!dev_ptr_ok(q) || !dev_ptr_ok(k) || !dev_ptr_ok(v) || !dev_ptr_ok(o) || !dev_ptr_ok(d_o) || !dev_ptr_ok(lse))
+    return MEA_ERR_INVALID_ARG;
+  if (o_lo && (!aligned16(o_lo) || p->dtype == MEA_F32)) return MEA_ERR_INVALID_ARG;
+  if (!aligned16(dq) || !aligned16(dk) || !aligned16(dv) || (dk == nullptr) != (dv == nullptr) || (!dq && !dk))
+    return MEA_ERR_INVALID_ARG;
+  if (d_table && (!aligned4(d_table) || !s->table || !dq)) return MEA_ERR_INVALID_ARG;
+  const BwdWork w = plan_scored_bwd(p, s);
+  if (!workspace || workspace_bytes < w.total) return MEA_ERR_WORKSPACE;
+  const int64_t kv = kv_heads_of(p, s->kv_heads);
+  ScoredBwdParams a = {};
+  a.s = score_args(p, s);
+  a.q = q;
+  a.k = k;
+  a.v = v;
+  a.o = o;
+  a.o_lo = o_lo;
+  a.d_o = d_o;
+  a.lse = lse;
+  a.dq = dq;
+  a.dk = dk;
+  a.dv = dv;
+  a.d_table = d_table;
+  a.n_q = p->n_q;
+  a.n_k = p->n_k;
+  a.n_q_pad = w.n_q_pad;
+  a.n_b = (int)p->batch;
+  a.heads_kv = (int)kv;
+  a.heads_per_kv = (int)(p->heads / kv);
+  a.scale = p->scale;
+  a.scale_log2 = p->scale * kLog2e;
+  {
+    const mea_strides* t = p->strides;
+    const size_t e = elem_size(p->dtype);
+    const int64_t d = p->d, B = p->batch, H = p->heads;
+    a.sq = strides_of(t ? &t->q : nullptr, H, p->n_q, d);
+    a.sk = strides_of(t ? &t->k : nullptr, kv, p->n_k, d);
+    a.sv = strides_of(t ? &t->v : nullptr, kv, p->n_k, d);
+    a.so = strides_of(t ? &t->o : nullptr, H, p->n_q, d);
+    a.sdo = strides_of(t ? &t->d_o : nullptr, H, p->n_q, d);
+    a.sdq = strides_of(t ? &t->dq : nullptr, H, p->n_q, d);
+    a.sdk = strides_of(t ? &t->dk : nullptr, kv, p->n_k, d);
+    a.sdv = strides_of(t ? &t->dv : nullptr, kv, p->n_k, d);
+    if (!strides_ok(B, H, a.sq, p->n_q, false, e, d) || !strides_ok(B, kv, a.sk, p->n_k, false, e, d) ||
+        !strides_ok(B, kv, a.sv, p->n_k, false, e, d) || !strides_ok(B, H, a.so, p->n_q, false, e, d) ||
+        !strides_ok(B, H, a.sdo, p->n_q, false, e, d) || (dq && !strides_ok(B, H, a.sdq, p->n_q, true, e, d)) ||
+        (dk && (!strides_ok(B, kv, a.sdk, p->n_k, true, e, d) || !strides_ok(B, kv, a.sdv, p->n_k, true, e, d))))
+      return MEA_ERR_INVALID_ARG;
+  }
+  if (!fits_launch(p->batch * p->heads * (w.n_q_pad / 8)) || !fits_launch(p->batch * kv * ((p->n_k + 127) / 128)))
+    return MEA_ERR_INVALID_ARG;
+  if (p->causal)
+    a.tile_order = mea::causal_tile_order(p->batch * kv * p->n_k * 2 * p->d * (int64_t)elem_size(p->dtype), 0, false);
+  float* at = align256(workspace, 0);
+  a.lse2 = at;
+  a.neg_d = at + w.rows / 4;
+  at += 2 * w.rows / 4;
+  if (s->q_doc) {
+    int2* rq = reinterpret_cast<int2*>(at);
+    int2* rk = reinterpret_cast<int2*>(at + w.ranges_q / 4);
+    a.s.q_range = rq;
+    a.s.k_range = rk;
+    at += (w.ranges_q + w.ranges_k) / 4;
+    hipError_t e = mea::launch_doc_ranges(s->q_doc, p->n_q, p->batch, rq, stream);
+    if (e == hipSuccess) e = mea::launch_doc_ranges(s->k_doc, p->n_k, p->batch, rk, stream);
+    if (e != hipSuccess) return MEA_ERR_HIP;
+  }
+  if (d_table) a.table_part = at;
+  const int d = (int)p->d;
+  switch (p->dtype) {
+    case MEA_F32: return status_of(mea::launch_scored_bwd<float>(a, d, stream));
+    case MEA_F16: return status_of(mea::launch_scored_bwd<_Float16>(a, d, stream));
+    default: return status_of(mea::launch_scored_bwd<__bf16>(a, d, stream));
+  }
+}
+
+mea_status mea_prefix_attention_fwd_workspace_size(const mea_problem* p, const mea_shared_prefix* x, size_t* bytes) {
+  const mea_status st = check_prefix(p, x);
+  if (st != MEA_OK) return st;
+  if (!bytes) return MEA_ERR_INVALID_ARG;
+  *bytes = plan_prefix(p, x).total;
+  return MEA_OK;
+}
+
+mea_status mea_prefix_attention_fwd(const mea_problem* p, const mea_shared_prefix* x, const void* q, const void* k,
+                                    const void* v, void* o, float* lse, void* workspace, size_t workspace_bytes,
+                                    hipStream_t stream) {
+  const mea_status st = check_prefix(p, x);
+  if (st != MEA_OK) return st;
+  if (!dev_ptr_ok(q) || !dev_ptr_ok(k) || !dev_ptr_ok(v) || !dev_ptr_ok(o) || !dev_ptr_ok(x->k) || !dev_ptr_ok(x->v))
+    return MEA_ERR_INVALID_ARG;
+  if (lse && !aligned16(lse)) return MEA_ERR_INVALID_ARG;
+  const PrefixWork w = plan_prefix(p, x);
+  if (!workspace || workspace_bytes < w.total) return MEA_ERR_WORKSPACE;
+  const int64_t kv = kv_heads_of(p, x->kv_heads), d = p->d;
+  const size_t e = elem_size(p->dtype);
+  ScoreArgs sa = score_args(p, nullptr);
+  sa.q_pos = x->q_pos;
+  StreamParams own = stream_params(p, sa, kv, w.own);
+  const mea_strides* t = p->strides;
+  own.q = q;
+  own.k = k;
+  own.v = v;
+  own.o = o;
+  own.lse = lse;
+  own.sq = strides_of(t ? &t->q : nullptr, p->heads, p->n_q, d);
+  own.sk = strides_of(t ? &t->k : nullptr, kv, p->n_k, d);
+  own.sv = strides_of(t ? &t->v : nullptr, kv, p->n_k, d);
+  own.so = strides_of(t ? &t->o : nullptr, p->heads, p->n_q, d);
+  auto shared_strides = [&](const mea_tensor_strides& s) {
+    return s.row ? mea::TensorStrides{0, s.head, s.row} : mea::TensorStrides{0, x->n_p * d, d};
+  };
+  const mea::TensorStrides spk = shared_strides(x->k_strides), spv = shared_strides(x->v_strides);
+  if (!strides_ok(p->batch, p->heads, own.sq, p->n_q, false, e, d) || !strides_ok(p->batch, kv, own.sk, p->n_k, false, e, d) ||
+      !strides_ok(p->batch, kv, own.sv, p->n_k, false, e, d) || !strides_ok(p->batch, p->heads, own.so, p->n_q, true, e, d) ||
+      !strides_ok(1, kv, spk, x->n_p, false, e, d) || !strides_ok(1, kv, spv, x->n_p, false, e, d))
+    return MEA_ERR_INVALID_ARG;
+  if (!fits_launch(w.own.rtiles * w.own.groups * w.own.splits) || !fits_launch(w.shared.rtiles * w.shared.groups * w.shared.splits) ||
+      !fits_launch((own.out_rows * d / 4 + 255) / 256))
+    return MEA_ERR_INVALID_ARG;
+  const int64_t parts = w.shared.splits + w.own.splits;
+  carve_parts(&own, p, parts, align256(workspace, 0));
+  own.split0 = (int)w.shared.splits;
+  StreamParams pre = stream_params(p, ScoreArgs{}, kv, w.shared);
+  pre.s.heads = (int)p->heads;
+  pre.q = q;
+  pre.sq = own.sq;
+  pre.k = x->k;
+  pre.v = x->v;
+  pre.sk = spk;
+  pre.sv = spv;
+  pre.n_k = x->n_p;
+  pre.batches = (int)p->batch;
+  pre.n_b = 1;
+  pre.part_o = own.part_o;
+  pre.part_m = own.part_m;
+  pre.part_l = own.part_l;
+  hipError_t err = run_stream(pre, p, w.shared.row_waves, stream);
+  if (err == hipSuccess) err = run_stream(own, p, w.own.row_waves, stream);
+  if (err == hipSuccess) err = run_combine(own, p, (int)parts, stream);
+  return status_of(err);
+}
+
+}  // extern "C"

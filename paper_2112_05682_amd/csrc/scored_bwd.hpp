@@ -1,0 +1,867 @@
+// Backward of attention with modified scores (scored.hpp), recomputing each tile's
+// scores from the forward's log-sum-exp (arXiv 2112.05682, Section 5.2):
+//   P_ij = exp(s_ij - lse_i),  dP_ij = dO_i . v_j,  D_i = dO_i . o_i,
+//   dS_ij = P_ij (dP_ij - D_i),              dV_j = sum_i P_ij dO_i,
+//   dX_ij = dS_ij (1 - (y_ij / cap)^2),      dK_j = scale sum_i dX_ij q_i,
+//   dtable[t, h] = sum dS_ij over the pairs  dQ_i = scale sum_j dX_ij k_j.
+//   of bucket t (all batches),
+// Three passes, and no atomics in memory, so that results do not depend on timing:
+//   pre  : lse and D of every row;
+//   dkdv : a wave per 32 keys of a key head (K, V in registers), over the queries of
+//          every head that shares it, so that shared heads' gradients add up in
+//          registers; a key on each lane;
+//   dq   : a wave per 32 queries (Q, dO in registers) over the keys; a query on each
+//          lane.  Its dS also gives the bias gradient: per lane one sum for each
+//          side beyond the span, and within it sums by distance in LDS.
+#pragma once
+
+#include "scored.hpp"
+
+namespace mea {
+
+// ------------------------------------------------------------------- pre
+template <typename T, int D>
+__global__ __launch_bounds__(256) void scored_bwd_pre_kernel(ScoredBwdParams p) {
+  constexpr int E = sizeof(T), W = 16 / E, TPR = D / W, RPB = 256 / TPR;
+  const int64_t rows = (int64_t)p.n_b * p.s.heads * p.n_q_pad;
+  const int64_t prow = (int64_t)blockIdx.x * RPB + threadIdx.x / TPR;
+  const int64_t bh = prow / p.n_q_pad, i = prow % p.n_q_pad;
+  const bool real = prow < rows && i < p.n_q;
+  const int part = threadIdx.x % TPR;
+  float acc = 0.0f;
+  if (real) {
+    typedef T vec __attribute__((ext_vector_type(W)));
+    const int64_t b = bh / p.s.heads, hd = bh % p.s.heads;
+    const vec o = *reinterpret_cast<const vec*>(static_cast<const T*>(p.o) + b * p.so.b + hd * p.so.h + i * p.so.r + part * W);
+    const vec g = *reinterpret_cast<const vec*>(static_cast<const T*>(p.d_o) + b * p.sdo.b + hd * p.sdo.h + i * p.sdo.r + part * W);
+    float of[W];
+#pragma unroll
+    for (int e = 0; e < W; ++e) of[e] = (float)o[e];
+    if constexpr (E == 2) {
+      // o + o_lo carries about 16 bits of the unrounded output; D is subtracted from
+      // sums it nearly equals, where o's own rounding would show.
+      if (p.o_lo) {
+        const vec lo = *reinterpret_cast<const vec*>(static_cast<const T*>(p.o_lo) + (bh * p.n_q + i) * D + part * W);
+#pragma unroll
+        for (int e = 0; e < W; ++e) of[e] += (float)lo[e];
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < W; ++e) acc = fmaf(of[e], (float)g[e], acc);
+  }
+#pragma unroll
+  for (int off = TPR / 2; off > 0; off >>= 1) acc += __shfl_xor(acc, off, TPR);
+  if (prow < rows && part == 0) {
+    const float lse = real ? p.lse[bh * p.n_q + i] : -INFINITY;
+    const bool live = lse != -INFINITY;
+    p.lse2[prow] = live ? lse * kLog2eF : INFINITY;
+    p.neg_d[prow] = live ? -acc : 0.0f;
+  }
+}
+
+// ------------------------------------------------------------------- dK, dV
+template <typename T, int D>
+struct ScoredKvTile {
+  static constexpr bool F32 = sizeof(T) == 4;
+  static constexpr int NT = 256, BKG = 128;              // keys of a workgroup
+  static constexpr int QS = D == 64 ? 2 : 1, BQ = 32 * QS;  // queries of a staged tile
+  static constexpr int NP = Planes<T>::NP;
+  static constexpr int RS = D + 8, TILE = BQ * RS;       // float32: padded rows of three planes
+  static constexpr int TILE_BYTES = F32 ? NP * TILE * 2 : BQ * D * 2;
+  static constexpr int STAGE_BYTES = 2 * TILE_BYTES + 2 * BQ * 4;  // Q, dO, lse2, -D
+  static constexpr int OCC = F32 ? 1 : 2;
+  // 16-bit, d = 128: the K fragments of every lane wait in LDS (32 registers less).
+  static constexpr bool K_LDS = !F32 && D == 128;
+  static constexpr int KSLOT_BYTES = K_LDS ? NT * (D / 16) * 16 : 0;
+  static constexpr int kBiasMax = 4 * (2 * kMaxBiasSpan + 1) + 16;
+  static constexpr int NBUF = 2 * STAGE_BYTES + KSLOT_BYTES + kBiasMax <= 160 * 1024 / OCC - 64 ? 2 : 1;
+  static constexpr int LDS_BYTES = NBUF * STAGE_BYTES + KSLOT_BYTES;
+  static constexpr int CPR = D / 8, CHUNKS = 2 * BQ * CPR, CPT = CHUNKS / NT;
+  static_assert(CHUNKS % NT == 0, "tile shapes");
+  static_assert(F32 || NBUF == 2, "asynchronous copies need two stages");
+};
+
+template <typename T, int D, bool CAP, bool BIAS>
+__global__ __launch_bounds__(256, (ScoredKvTile<T, D>::OCC)) void scored_dkdv_kernel(ScoredBwdParams p) {
+  using C = ScoredKvTile<T, D>;
+  using LE = typename Planes<T>::E;
+  constexpr bool F32 = C::F32, LOG2 = CAP || BIAS;
+  constexpr int BQ = C::BQ, QS = C::QS, KC = D / 16, NDT = D / 32, NBUF = C::NBUF;
+
+  extern __shared__ __align__(16) unsigned char smem[];
+  unsigned char* const lds_bias = smem + C::LDS_BYTES;
+  __shared__ int4 wave_ids[4];
+
+  const ScoreArgs& sa = p.s;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+  const int h = lane >> 5, c = lane & 31;
+
+  const TileItem item = tile_item(blockIdx.x, gridDim.x, p.n_ktiles, sa.causal ? p.tile_order : 0);
+  const int b = item.group % p.n_b, kvh = item.group / p.n_b;
+  const int64_t k0 = (int64_t)item.tile * C::BKG, kw = k0 + 32 * wave, key = kw + c;
+
+  const int64_t n_kv = batch_keys(sa, b, p.n_k), pos0 = first_pos(sa, b);
+  const int64_t reach = sa.causal ? (sa.prefix ? (int64_t)sa.prefix[b] : 0) : p.n_k;  // keys that every query sees
+  bool live = key < n_kv;
+  int doc = -2;
+  int4 ids = make_int4(0, 0, 0, 0);
+  if (sa.q_doc) {
+    doc = key < p.n_k ? sa.k_doc[(int64_t)b * p.n_k + key] : -1;
+    if (doc < 0) {
+      doc = -2;
+      live = false;
+    }
+    ids = workgroup_ids(doc, wave, lane, wave_ids);
+  }
+  // The first query that sees this lane's key, and (uniform) the first one of the
+  // workgroup's first key, of its last, and of the wave's first.
+  auto first_query = [&](int64_t j) { return j < reach || j <= pos0 ? (int64_t)0 : j - pos0; };
+  const int64_t min_q = live ? first_query(key) : p.n_q;
+  const int64_t q_begin = first_query(k0), q_full = first_query(k0 + C::BKG - 1), qw_begin = first_query(kw);
+  const bool all_live = k0 + C::BKG <= n_kv && ids.z == 0;
+
+  const T* __restrict__ kg = static_cast<const T*>(p.k) + (int64_t)b * p.sk.b + (int64_t)kvh * p.sk.h;
+  const T* __restrict__ vg = static_cast<const T*>(p.v) + (int64_t)b * p.sv.b + (int64_t)kvh * p.sv.h;
+
+  // K^T and V^T as B operands: lane (h, key c) holds features 16 kc + 8 h ..
+  Range<T, false> range;
+  T* const kslot = reinterpret_cast<T*>(smem + NBUF * C::STAGE_BYTES) + 8 * tid;
+  Frag<T> kf[C::K_LDS ? 1 : KC], vf[KC];
+#pragma unroll
+  for (int kc = 0; kc < KC; ++kc) {
+    const Frag<T> f = live ? ld_frag_as<T, T>(kg + key * p.sk.r + 16 * kc + 8 * h, range) : zero_frag<T>();
+    if constexpr (C::K_LDS) *reinterpret_cast<Frag<T>*>(kslot + 8 * C::NT * kc) = f;
+    else kf[kc] = f;
+    vf[kc] = live ? ld_frag_as<T, T>(vg + key * p.sv.r + 16 * kc + 8 * h, range) : zero_frag<T>();
+  }
+  auto kfrag = [&](int kc) __attribute__((always_inline)) {
+    if constexpr (C::K_LDS) return lds_frag<T>(kslot + 8 * C::NT * kc);
+    else return kf[kc];
+  };
+
+  f32x16 dk[NDT], dv[NDT];
+#pragma unroll
+  for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) dk[dt][r] = dv[dt][r] = 0.0f;
+  wait_global_loads();
+
+  // ---- the stream: for each head of the key head its query tiles.
+  const int n_units = (int)((p.n_q + 31) / 32);
+  const int2* const ranges = sa.q_range ? sa.q_range + (int64_t)b * n_units : nullptr;
+  DocTiles<QS> docs(ranges, n_units, ids.x, ids.y);
+  const int t_end = k0 < n_kv ? (int)((p.n_q + BQ - 1) / BQ) : 0;
+  int g = 0, t = 0;  // current head and tile
+  auto first_tile = [&]() {
+    docs.base = -64;
+    const int64_t f = q_begin / BQ;
+    return docs.next(f < t_end ? (int)f : t_end, t_end);
+  };
+  // The tile after (g_, t_); g_ = heads_per_kv at the end.
+  auto advance = [&](int& g_, int& t_) {
+    t_ = docs.next(t_ + 1, t_end);
+    if (t_ >= t_end) {
+      ++g_;
+      t_ = first_tile();
+    }
+  };
+  t = first_tile();
+  if (t >= t_end) g = p.heads_per_kv;  // no query sees these keys
+
+  constexpr int CPR = C::CPR, RPU = 64 / CPR, UPW = F32 ? 1 : BQ / RPU / 4;
+  const int urow = lane / CPR, uch = lane % CPR;
+  auto head_of = [&](int g_) { return kvh * p.heads_per_kv + g_; };
+  float stage_f = 0.0f;
+  auto load_rows = [&](int g_, int t_) __attribute__((always_inline)) {
+    if (tid < 2 * BQ) {
+      const int64_t at = ((int64_t)b * sa.heads + head_of(g_)) * p.n_q_pad + (int64_t)t_ * BQ + tid % BQ;
+      stage_f = tid < BQ ? p.lse2[at] : p.neg_d[at];
+    }
+  };
+  auto store_rows = [&](int buf) __attribute__((always_inline)) {
+    if (tid < 2 * BQ) reinterpret_cast<float*>(smem + buf * C::STAGE_BYTES + 2 * C::TILE_BYTES)[tid] = stage_f;
+  };
+  // 16-bit: asynchronous copies into swizzled rows; rows past n_q repeat the last.
+  auto copy_tile = [&](int g_, int t_, int buf) __attribute__((always_inline)) {
+    const T* qg = static_cast<const T*>(p.q) + (int64_t)b * p.sq.b + (int64_t)head_of(g_) * p.sq.h;
+    const T* og = static_cast<const T*>(p.d_o) + (int64_t)b * p.sdo.b + (int64_t)head_of(g_) * p.sdo.h;
+    const unsigned base = __builtin_amdgcn_readfirstlane(lds_addr(smem + buf * C::STAGE_BYTES));
+#pragma unroll
+    for (int j = 0; j < UPW; ++j) {
+      const int u = wave + 4 * j, r = RPU * u + urow;
+      int64_t qi = (int64_t)t_ * BQ + r;
+      if (qi > p.n_q - 1) qi = p.n_q - 1;
+      const int ch = 8 * (uch ^ swz<D>(r));
+      copy_to_lds16(qg + qi * p.sq.r + ch, base + 1024u * (unsigned)u);
+      copy_to_lds16(og + qi * p.sdo.r + ch, base + (unsigned)C::TILE_BYTES + 1024u * (unsigned)u);
+    }
+  };
+  Chunk8<T> stage[F32 ? C::CPT : 1];
+  auto load_stage = [&](int g_, int t_) __attribute__((always_inline)) {
+    if constexpr (F32) {
+      const T* qg = static_cast<const T*>(p.q) + (int64_t)b * p.sq.b + (int64_t)head_of(g_) * p.sq.h;
+      const T* og = static_cast<const T*>(p.d_o) + (int64_t)b * p.sdo.b + (int64_t)head_of(g_) * p.sdo.h;
+#pragma unroll
+      for (int i = 0; i < C::CPT; ++i) {
+        const int chunk = tid + i * C::NT;
+        const bool is_o = chunk >= BQ * CPR;
+        const int rem = is_o ? chunk - BQ * CPR : chunk;
+        const int r = rem / CPR, col = rem % CPR;
+        const int64_t qi = (int64_t)t_ * BQ + r;
+        const T* src = is_o ? og + qi * p.sdo.r : qg + qi * p.sq.r;
+        stage[i] = qi < p.n_q ? ld_chunk8<T, T>(src + 8 * col) : zero_chunk8<T>();
+      }
+    }
+  };
+  auto store_stage = [&](int buf) __attribute__((always_inline)) {
+    if constexpr (F32) {
+#pragma unroll
+      for (int i = 0; i < C::CPT; ++i) {
+        const int chunk = tid + i * C::NT;
+        const bool is_o = chunk >= BQ * CPR;
+        const int rem = is_o ? chunk - BQ * CPR : chunk;
+        st_chunk8<T>(reinterpret_cast<LE*>(smem + buf * C::STAGE_BYTES + (is_o ? C::TILE_BYTES : 0)) + rem / CPR * C::RS +
+                         8 * (rem % CPR),
+                     C::TILE, stage[i], range);
+      }
+    }
+  };
+
+  const int qrow = perm32(c);
+  const float cl2 = p.scale_log2;
+  float slope2 = 0.0f;
+
+  auto compute = [&](auto mask_tag, int t_, int buf, bool one_doc) {
+    constexpr bool MASK = decltype(mask_tag)::value;
+    const int64_t q0t = (int64_t)t_ * BQ;
+    if (q0t + BQ <= qw_begin || kw >= n_kv) return;  // none of the wave's keys is seen
+    const unsigned char* st = smem + buf * C::STAGE_BYTES;
+    const float* lse_s = reinterpret_cast<const float*>(st + 2 * C::TILE_BYTES);
+    const float* nd_s = lse_s + BQ;
+#pragma unroll
+    for (int qs = 0; qs < QS; ++qs) {
+      const int64_t q0 = q0t + 32 * qs;
+      const unsigned char* qt = st + qs * 32 * (2 * D);
+      const unsigned char* ot = qt + C::TILE_BYTES;
+      const LE* qt32 = reinterpret_cast<const LE*>(st) + qs * 32 * C::RS;
+      const LE* ot32 = reinterpret_cast<const LE*>(st + C::TILE_BYTES) + qs * 32 * C::RS;
+      f32x16 s, dp;
+      float l2[16];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int row = 32 * qs + 16 * (j >> 1) + 8 * h + 4 * (j & 1);
+        const f32x4 a = *reinterpret_cast<const f32x4*>(lse_s + row);
+        const f32x4 d = *reinterpret_cast<const f32x4*>(nd_s + row);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          s[4 * j + e] = 0.0f;
+          l2[4 * j + e] = a[e];
+          dp[4 * j + e] = d[e];
+        }
+      }
+#pragma unroll
+      for (int kc = 0; kc < KC; ++kc) {
+        if constexpr (F32) {
+          s = mma(lds_frag_planes<T>(qt32 + qrow * C::RS + 16 * kc + 8 * h, C::TILE), kfrag(kc), s);
+          dp = mma(lds_frag_planes<T>(ot32 + qrow * C::RS + 16 * kc + 8 * h, C::TILE), vf[kc], dp);
+        } else {
+          s = mma(row_frag<T, D>(qt, qrow, 2 * kc + h), kfrag(kc), s);
+          dp = mma(row_frag<T, D>(ot, qrow, 2 * kc + h), vf[kc], dp);
+        }
+      }
+      float grad[CAP ? 16 : 1];  // 1 - tanh^2
+      if constexpr (LOG2) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          if constexpr (CAP) {
+            const float th = cap_tanh<T>(sa, s[r]);
+            grad[r] = fmaf(-th, th, 1.0f);
+            s[r] = sa.cap2 * th;
+          } else {
+            s[r] *= cl2;
+          }
+        }
+      }
+      if constexpr (BIAS) {
+        const int off = rel(key - (pos0 + q0));  // distance to the tile's first query
+        if (sa.slopes) {
+          const float d0 = (float)off;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[r] = fmaf(-fabsf(d0 - (float)permuted_row(r, h)), slope2, s[r]);
+        }
+        if (sa.table) {
+          const int hi = sa.two_sided ? sa.span : 0, last = bias_places(sa) - 1;
+          const int64_t p_lo = pos0 + q0, p_hi = p_lo + 31;
+          if (kw + 31 <= p_lo - sa.span || kw >= p_hi + hi) {
+            const float x = reinterpret_cast<const float*>(lds_bias)[kw >= p_hi + hi ? last : 0];
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[r] += x;
+          } else {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+              int d = off - permuted_row(r, h);
+              d = d < -sa.span ? -sa.span : (d > hi ? hi : d);
+              s[r] += reinterpret_cast<const float*>(lds_bias)[d + sa.span];
+            }
+          }
+        }
+      }
+      // P and dS; absent: rows without a document (bit 8 m + e: row 16 m + 8 h + e).
+      uint32_t absent = 0;
+      float pr[16];
+#pragma unroll
+      for (int r = 0; r < 16; ++r) pr[r] = fast_exp2(LOG2 ? s[r] - l2[r] : fmaf(s[r], cl2, -l2[r]));
+      if constexpr (MASK) {
+        const int m = rel(min_q - q0);
+        int mine = 0;
+        const bool by_doc = sa.q_doc && !one_doc;
+        if (by_doc) mine = q0 + c < p.n_q ? sa.q_doc[(int64_t)b * p.n_q + q0 + c] : -1;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          bool off_ = permuted_row(r, h) < m;
+          if (by_doc) {
+            const int id = __shfl(mine, permuted_row(r, h));
+            off_ = off_ || id != doc;
+            if (id < 0) absent |= 1u << r;
+          }
+          pr[r] = off_ ? 0.0f : pr[r];
+          dp[r] = off_ ? 0.0f : pr[r] * dp[r];
+          if constexpr (CAP) grad[r] = off_ ? 0.0f : grad[r];  // a hidden score may be NaN
+        }
+      } else {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) dp[r] *= pr[r];
+      }
+      if constexpr (CAP)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) dp[r] *= grad[r];
+      const bool drop = MASK && __builtin_amdgcn_ballot_w64(absent != 0);
+      // dV^T += dO^T P and dK^T += Q^T dX.
+      Frag<T> pf[2], sf[2];
+#pragma unroll
+      for (int m = 0; m < 2; ++m) {
+        float x[8], y[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          x[e] = pr[8 * m + e];
+          y[e] = dp[8 * m + e];
+        }
+        pf[m] = to_frag<T>(x);
+        sf[m] = to_frag<T>(y);
+      }
+#pragma unroll
+      for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+          Frag<T> a, e;
+          if constexpr (F32) {
+            a = lds_col_frag_planes<T>(ot32, C::TILE, C::RS, 16 * m, 32 * dt, lane);
+            e = lds_col_frag_planes<T>(qt32, C::TILE, C::RS, 16 * m, 32 * dt, lane);
+          } else {
+            a = col_frag<T, D>(ot, 16 * m, 32 * dt, lane);
+            e = col_frag<T, D>(qt, 16 * m, 32 * dt, lane);
+          }
+          if constexpr (MASK)
+            if (drop) {
+              a = without<T>(a, absent >> (8 * m));
+              e = without<T>(e, absent >> (8 * m));
+            }
+          dv[dt] = mma(a, pf[m], dv[dt]);
+          dk[dt] = mma(e, sf[m], dk[dt]);
+        }
+    }
+  };
+
+  int buf = 0, g_bias = -1;
+  if (g < p.heads_per_kv) {
+    load_rows(g, t);
+    if constexpr (F32) {
+      load_stage(g, t);
+      store_stage(0);
+    } else {
+      copy_tile(g, t, 0);
+    }
+    store_rows(0);
+  }
+  if constexpr (F32) __syncthreads();
+  while (g < p.heads_per_kv) {
+    const bool one_doc = ids.z == 0 && docs.uniform(t);
+    const bool plain = all_live && one_doc && (int64_t)t * BQ >= q_full;
+    int gn = g, tn = t;
+    advance(gn, tn);
+    const bool more = gn < p.heads_per_kv;
+    if constexpr (!F32) {
+      wait_global_loads();
+      __syncthreads();
+    }
+    if constexpr (BIAS) {
+      if (g != g_bias) {  // the heads' biases take turns
+        if (sa.slopes) slope2 = sa.slopes[head_of(g)] * kLog2eF;
+        if (sa.table) {
+          fill_bias(sa, lds_bias, 1, head_of(g), tid, C::NT);
+          __syncthreads();
+        }
+        g_bias = g;
+      }
+    }
+    if (more) {
+      load_rows(gn, tn);
+      if constexpr (F32) load_stage(gn, tn);
+      else copy_tile(gn, tn, buf ^ 1);
+    }
+    if (plain) compute(std::false_type{}, t, buf, true);
+    else compute(std::true_type{}, t, buf, one_doc);
+    const int nb = NBUF == 2 ? buf ^ 1 : 0;
+    if constexpr (F32) {
+      if (NBUF == 1) __syncthreads();
+      if (more) {
+        store_stage(nb);
+        store_rows(nb);
+      }
+      __syncthreads();
+    } else {
+      if (more) store_rows(nb);
+    }
+    buf = nb;
+    g = gn;
+    t = tn;
+  }
+
+  if (key >= p.n_k) return;
+  T* dkg = static_cast<T*>(p.dk) + (int64_t)b * p.sdk.b + (int64_t)kvh * p.sdk.h + key * p.sdk.r;
+  T* dvg = static_cast<T*>(p.dv) + (int64_t)b * p.sdv.b + (int64_t)kvh * p.sdv.h + key * p.sdv.r;
+#pragma unroll
+  for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+    for (int a4 = 0; a4 < 4; ++a4) {
+      typename FragT<T>::half x, y;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        x[e] = (T)(live ? dk[dt][4 * a4 + e] * p.scale : 0.0f);
+        y[e] = (T)(live ? dv[dt][4 * a4 + e] : 0.0f);
+      }
+      *reinterpret_cast<typename FragT<T>::half*>(dkg + 32 * dt + 8 * a4 + 4 * h) = x;
+      *reinterpret_cast<typename FragT<T>::half*>(dvg + 32 * dt + 8 * a4 + 4 * h) = y;
+    }
+}
+
+// ------------------------------------------------------------------- dQ
+template <typename T, int D>
+struct ScoredDqTile {
+  static constexpr bool F32 = sizeof(T) == 4;
+  static constexpr int NT = 256, ROWS = kScoredDqRows;
+  static constexpr int BK = !F32 && D == 64 ? 64 : 32;
+  static constexpr int NP = Planes<T>::NP;
+  static constexpr int RS = D + 8, TILE = BK * RS;
+  static constexpr int TILE_BYTES = F32 ? NP * TILE * 2 : BK * D * 2;
+  static constexpr int STAGE_BYTES = 2 * TILE_BYTES;
+  static constexpr int OCC = F32 && D == 128 ? 1 : 2;
+  // The bias by place and, for its gradient, sums by place of each wave and half.
+  static constexpr int kBiasMax = 4 * (2 * kMaxBiasSpan + 1) + 16;
+  static constexpr int NBUF = 2 * STAGE_BYTES + 9 * kBiasMax <= 160 * 1024 / OCC - 256 ? 2 : 1;
+  static constexpr int LDS_BYTES = NBUF * STAGE_BYTES;
+  static constexpr int CPR = D / 8, CHUNKS = 2 * BK * CPR, CPT = CHUNKS / NT;
+  static_assert(CHUNKS % NT == 0, "tile shapes");
+  static_assert(F32 || NBUF == 2, "asynchronous copies need two stages");
+};
+
+__device__ __forceinline__ void lds_add(float* p, float x) {
+  __hip_atomic_fetch_add(p, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+}
+
+template <typename T, int D, bool CAP, bool BIAS>
+__global__ __launch_bounds__(256, (ScoredDqTile<T, D>::OCC)) void scored_dq_kernel(ScoredBwdParams p) {
+  using C = ScoredDqTile<T, D>;
+  using LE = typename Planes<T>::E;
+  constexpr bool F32 = C::F32, LOG2 = CAP || BIAS;
+  constexpr int BK = C::BK, KC = D / 16, NKT = BK / 32, NDT = D / 32, NBUF = C::NBUF;
+
+  extern __shared__ __align__(16) unsigned char smem[];
+  unsigned char* const lds_bias = smem + C::LDS_BYTES;
+  __shared__ int4 wave_ids[4];
+  __shared__ float far_sums[8];
+
+  const ScoreArgs& sa = p.s;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+  const int h = lane >> 5, c = lane & 31;
+
+  const TileItem item = tile_item(blockIdx.x, gridDim.x, p.n_qtiles, sa.causal ? p.tile_order : 0);
+  const int qtile = sa.causal ? p.n_qtiles - 1 - item.tile : item.tile;
+  // Heads that share a key head are neighbours, then batches.
+  const int gi = item.group / p.heads_per_kv;
+  const int b = gi % p.n_b, kvh = gi / p.n_b, head = kvh * p.heads_per_kv + item.group % p.heads_per_kv;
+  const int64_t q0 = (int64_t)qtile * C::ROWS, qw = q0 + 32 * wave, qi = qw + c;
+  const int64_t q_last = (q0 + C::ROWS < p.n_q ? q0 + C::ROWS : p.n_q) - 1;
+
+  const int64_t n_kv = batch_keys(sa, b, p.n_k), pos0 = first_pos(sa, b);
+  const int64_t row = ((int64_t)b * sa.heads + head) * p.n_q_pad + qi;
+  const bool in_rows = qi < p.n_q;
+  const float l2 = in_rows ? p.lse2[row] : INFINITY, neg_d = in_rows ? p.neg_d[row] : 0.0f;
+  int64_t lim = in_rows && l2 != INFINITY ? key_limit(sa, b, n_kv, pos0 + qi) : 0;
+  const int64_t lim_hi = key_limit(sa, b, n_kv, pos0 + q_last), lim_lo = key_limit(sa, b, n_kv, pos0 + q0);
+  const int64_t w_last = qw + 31 < p.n_q ? qw + 31 : p.n_q - 1;
+  const int64_t w_lim = qw < p.n_q ? key_limit(sa, b, n_kv, pos0 + w_last) : 0;
+
+  int doc = -2;
+  int4 ids = make_int4(0, 0, 0, 0);
+  if (sa.q_doc) {
+    doc = in_rows ? sa.q_doc[(int64_t)b * p.n_q + qi] : -1;
+    if (doc < 0) {
+      doc = -2;
+      lim = 0;
+    }
+    ids = workgroup_ids(doc, wave, lane, wave_ids);
+  }
+  const bool live = lim > 0;
+  const int n_units = (int)((p.n_k + 31) / 32);
+  DocTiles<BK / 32> docs(sa.k_range ? sa.k_range + (int64_t)b * n_units : nullptr, n_units, ids.x, ids.y);
+
+  const float slope2 = BIAS && sa.slopes ? sa.slopes[head] * kLog2eF : 0.0f;
+  const int places = BIAS ? bias_places(sa) : 0;
+  const bool sums = BIAS && p.table_part;
+  // Sums by place, of each wave and lane half (their lanes of one instruction have
+  // places of their own, so that the order of the additions is fixed).
+  float* const bins = reinterpret_cast<float*>(lds_bias + bias_lds_bytes(sa, 1));
+  float* const my_bins = bins + (2 * wave + h) * places;
+  if (BIAS && sa.table) {
+    fill_bias(sa, lds_bias, 1, head, tid, C::NT);
+    if (sums)
+      for (int x = tid; x < 8 * places; x += C::NT) bins[x] = 0.0f;
+  }
+
+  const T* __restrict__ kg = static_cast<const T*>(p.k) + (int64_t)b * p.sk.b + (int64_t)kvh * p.sk.h;
+  const T* __restrict__ vg = static_cast<const T*>(p.v) + (int64_t)b * p.sv.b + (int64_t)kvh * p.sv.h;
+  Range<T, false> range;
+  Frag<T> qf[KC], gf[KC];
+  {
+    const T* qg = static_cast<const T*>(p.q) + (int64_t)b * p.sq.b + (int64_t)head * p.sq.h + qi * p.sq.r;
+    const T* og = static_cast<const T*>(p.d_o) + (int64_t)b * p.sdo.b + (int64_t)head * p.sdo.h + qi * p.sdo.r;
+#pragma unroll
+    for (int kc = 0; kc < KC; ++kc) {
+      qf[kc] = live ? ld_frag_as<T, T>(qg + 16 * kc + 8 * h, range) : zero_frag<T>();
+      gf[kc] = live ? ld_frag_as<T, T>(og + 16 * kc + 8 * h, range) : zero_frag<T>();
+    }
+  }
+  f32x16 acc[NDT];
+#pragma unroll
+  for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) acc[dt][r] = 0.0f;
+  float far_lo = 0.0f, far_hi = 0.0f;
+  wait_global_loads();
+  __syncthreads();  // the bias is there
+
+  constexpr int CPR = C::CPR, RPU = 64 / CPR, UPW = F32 ? 1 : BK / RPU / 4;
+  const int urow = lane / CPR, uch = lane % CPR;
+  auto copy_tile = [&](int t, int buf) __attribute__((always_inline)) {
+    const unsigned base = __builtin_amdgcn_readfirstlane(lds_addr(smem + buf * C::STAGE_BYTES));
+#pragma unroll
+    for (int j = 0; j < UPW; ++j) {
+      const int u = wave + 4 * j, r = RPU * u + urow;
+      int64_t key = (int64_t)t * BK + r;
+      if (key > lim_hi - 1) key = lim_hi - 1;
+      const int ch = 8 * (uch ^ swz<D>(r));
+      copy_to_lds16(kg + key * p.sk.r + ch, base + 1024u * (unsigned)u);
+      copy_to_lds16(vg + key * p.sv.r + ch, base + (unsigned)C::TILE_BYTES + 1024u * (unsigned)u);
+    }
+  };
+  Chunk8<T> stage[F32 ? C::CPT : 1];
+  auto load_stage = [&](int t) __attribute__((always_inline)) {
+    if constexpr (F32) {
+#pragma unroll
+      for (int i = 0; i < C::CPT; ++i) {
+        const int chunk = tid + i * C::NT;
+        const bool is_v = chunk >= BK * CPR;
+        const int rem = is_v ? chunk - BK * CPR : chunk;
+        const int r = rem / CPR, col = rem % CPR;
+        const int64_t key = (int64_t)t * BK + r;
+        const T* src = is_v ? vg + key * p.sv.r : kg + key * p.sk.r;
+        stage[i] = key < lim_hi ? ld_chunk8<T, T>(src + 8 * col) : zero_chunk8<T>();
+      }
+    }
+  };
+  auto store_stage = [&](int buf) __attribute__((always_inline)) {
+    if constexpr (F32) {
+#pragma unroll
+      for (int i = 0; i < C::CPT; ++i) {
+        const int chunk = tid + i * C::NT;
+        const bool is_v = chunk >= BK * CPR;
+        const int rem = is_v ? chunk - BK * CPR : chunk;
+        st_chunk8<T>(reinterpret_cast<LE*>(smem + buf * C::STAGE_BYTES + (is_v ? C::TILE_BYTES : 0)) + rem / CPR * C::RS +
+                         8 * (rem % CPR),
+                     C::TILE, stage[i], range);
+      }
+    }
+  };
+
+  const int krow = perm32(c);
+  const float cl2 = p.scale_log2;
+  const int64_t p_lo = pos0 + qw, p_hi = pos0 + w_last;  // the wave's positions
+
+  auto tile = [&](auto mask_tag, int t, int buf, bool one_doc) {
+    constexpr bool MASK = decltype(mask_tag)::value;
+    const unsigned char* st = smem + buf * C::STAGE_BYTES;
+#pragma unroll
+    for (int kt = 0; kt < NKT; ++kt) {
+      const int64_t k0 = (int64_t)t * BK + 32 * kt;
+      if (k0 >= w_lim) return;
+      const unsigned char* kt16 = st + kt * 32 * (2 * D);
+      const unsigned char* vt16 = kt16 + C::TILE_BYTES;
+      const LE* kt32 = reinterpret_cast<const LE*>(st) + kt * 32 * C::RS;
+      const LE* vt32 = reinterpret_cast<const LE*>(st + C::TILE_BYTES) + kt * 32 * C::RS;
+      f32x16 s, dp;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        s[r] = 0.0f;
+        dp[r] = neg_d;
+      }
+#pragma unroll
+      for (int kc = 0; kc < KC; ++kc) {
+        if constexpr (F32) {
+          s = mma(lds_frag_planes<T>(kt32 + krow * C::RS + 16 * kc + 8 * h, C::TILE), qf[kc], s);
+          dp = mma(lds_frag_planes<T>(vt32 + krow * C::RS + 16 * kc + 8 * h, C::TILE), gf[kc], dp);
+        } else {
+          s = mma(row_frag<T, D>(kt16, krow, 2 * kc + h), qf[kc], s);
+          dp = mma(row_frag<T, D>(vt16, krow, 2 * kc + h), gf[kc], dp);
+        }
+      }
+      float grad[CAP ? 16 : 1];
+      if constexpr (LOG2) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          if constexpr (CAP) {
+            const float th = cap_tanh<T>(sa, s[r]);
+            grad[r] = fmaf(-th, th, 1.0f);
+            s[r] = sa.cap2 * th;
+          } else {
+            s[r] *= cl2;
+          }
+        }
+      }
+      const int off = BIAS ? rel(k0 - (pos0 + qi)) : 0;
+      const int hi = sa.two_sided ? sa.span : 0;
+      const bool far = BIAS && (k0 + 31 <= p_lo - sa.span || k0 >= p_hi + hi);
+      if constexpr (BIAS) {
+        if (sa.slopes) {
+          const float d0 = (float)off;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[r] = fmaf(-fabsf(d0 + (float)permuted_row(r, h)), slope2, s[r]);
+        }
+        if (sa.table) {
+          if (far) {
+            const float x = reinterpret_cast<const float*>(lds_bias)[k0 >= p_hi + hi ? places - 1 : 0];
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[r] += x;
+          } else {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+              int d = off + permuted_row(r, h);
+              d = d < -sa.span ? -sa.span : (d > hi ? hi : d);
+              s[r] += reinterpret_cast<const float*>(lds_bias)[d + sa.span];
+            }
+          }
+        }
+      }
+      uint32_t absent = 0;
+      float pr[16];
+#pragma unroll
+      for (int r = 0; r < 16; ++r) pr[r] = fast_exp2(LOG2 ? s[r] - l2 : fmaf(s[r], cl2, -l2));
+      if constexpr (MASK) {
+        const int m = rel(lim - k0);
+        int mine = 0;
+        const bool by_doc = sa.q_doc && !one_doc;
+        if (by_doc) mine = k0 + c < p.n_k ? sa.k_doc[(int64_t)b * p.n_k + k0 + c] : -1;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          bool off_ = permuted_row(r, h) >= m;
+          if (by_doc) {
+            const int id = __shfl(mine, permuted_row(r, h));
+            off_ = off_ || id != doc;
+            if (id < 0) absent |= 1u << r;
+          }
+          dp[r] = off_ ? 0.0f : pr[r] * dp[r];
+          if constexpr (CAP) grad[r] = off_ ? 0.0f : grad[r];  // a hidden score may be NaN
+        }
+      } else {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) dp[r] *= pr[r];
+      }
+      if constexpr (BIAS) {
+        if (sums) {
+          if (far) {
+            float y[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[e] = dp[e] + dp[8 + e];
+            const float x = tree_sum<8>(y, 0.0f);
+            if (k0 >= p_hi + hi) far_hi += x;
+            else far_lo += x;
+          } else {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+              const int d = off + permuted_row(r, h);
+              if (d <= -sa.span) far_lo += dp[r];
+              else if (d >= hi) far_hi += dp[r];
+              else lds_add(my_bins + d + sa.span, dp[r]);
+            }
+          }
+        }
+      }
+      if constexpr (CAP)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) dp[r] *= grad[r];
+      const bool drop = MASK && __builtin_amdgcn_ballot_w64(absent != 0);
+      Frag<T> sf[2];
+#pragma unroll
+      for (int m = 0; m < 2; ++m) {
+        float x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = dp[8 * m + e];
+        sf[m] = to_frag<T>(x);
+      }
+#pragma unroll
+      for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+          Frag<T> a;
+          if constexpr (F32) a = lds_col_frag_planes<T>(kt32, C::TILE, C::RS, 16 * m, 32 * dt, lane);
+          else a = col_frag<T, D>(kt16, 16 * m, 32 * dt, lane);
+          if constexpr (MASK)
+            if (drop) a = without<T>(a, absent >> (8 * m));
+          acc[dt] = mma(a, sf[m], acc[dt]);
+        }
+    }
+  };
+
+  const int t_end = (int)((lim_hi + BK - 1) / BK);
+  int t = docs.next(0, t_end), buf = 0;
+  if (t < t_end) {
+    if constexpr (F32) {
+      load_stage(t);
+      store_stage(0);
+    } else {
+      copy_tile(t, 0);
+    }
+  }
+  if constexpr (F32) __syncthreads();
+  while (t < t_end) {
+    const int tn = docs.next(t + 1, t_end);
+    const bool one_doc = ids.z == 0 && docs.uniform(t);
+    const bool plain = (int64_t)(t + 1) * BK <= lim_lo && one_doc;
+    if constexpr (F32) {
+      if (tn < t_end) load_stage(tn);
+    } else {
+      wait_global_loads();
+      __syncthreads();
+      if (tn < t_end) copy_tile(tn, buf ^ 1);
+    }
+    if (plain) tile(std::false_type{}, t, buf, true);
+    else tile(std::true_type{}, t, buf, one_doc);
+    const int nb = NBUF == 2 ? buf ^ 1 : 0;
+    if constexpr (F32) {
+      if (NBUF == 1) __syncthreads();
+      if (tn < t_end) store_stage(nb);
+      __syncthreads();
+    }
+    buf = nb;
+    t = tn;
+  }
+
+  if (in_rows) {
+    T* dqg = static_cast<T*>(p.dq) + (int64_t)b * p.sdq.b + (int64_t)head * p.sdq.h + qi * p.sdq.r;
+#pragma unroll
+    for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+      for (int a4 = 0; a4 < 4; ++a4) {
+        typename FragT<T>::half x;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = (T)(live ? acc[dt][4 * a4 + e] * p.scale : 0.0f);
+        *reinterpret_cast<typename FragT<T>::half*>(dqg + 32 * dt + 8 * a4 + 4 * h) = x;
+      }
+  }
+
+  if constexpr (BIAS) {
+    if (!sums) return;
+    // The workgroup's sums by bucket: waves and halves in order, then a bucket's places
+    // in order, the ends beyond the span with the far sums.
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+      far_lo += __shfl_xor(far_lo, o);
+      far_hi += __shfl_xor(far_hi, o);
+    }
+    if (lane == 0) {
+      far_sums[wave] = far_lo;
+      far_sums[4 + wave] = far_hi;
+    }
+    __syncthreads();
+    for (int x = tid; x < places; x += C::NT) {
+      float y = bins[x];
+#pragma unroll
+      for (int w = 1; w < 8; ++w) y += bins[w * places + x];
+      if (x == 0) y += (far_sums[0] + far_sums[1]) + (far_sums[2] + far_sums[3]);
+      if (x == places - 1) y += (far_sums[4] + far_sums[5]) + (far_sums[6] + far_sums[7]);
+      bins[x] = y;
+    }
+    __syncthreads();
+    const int nb = sa.n_edges * (sa.two_sided ? 2 : 1);
+    // Workgroups of one head are neighbours in table_part: [head][batch][query tile].
+    float* part = p.table_part + (((int64_t)head * p.n_b + b) * p.n_qtiles + qtile) * nb;
+    for (int e = tid; e < nb; e += C::NT) {
+      const bool ahead = e >= sa.n_edges;
+      const int s = ahead ? e - sa.n_edges : e;
+      int lo = sa.edges[s], end = s + 1 < sa.n_edges ? sa.edges[s + 1] : sa.span + 1;  // distances [lo, end)
+      if (end > sa.span + 1) end = sa.span + 1;
+      if (ahead && lo == 0) lo = 1;  // distance 0 is behind
+      float y = 0.0f;
+      for (int d = lo; d < end; ++d) y += bins[sa.span + (ahead ? d : -d)];
+      part[e] = y;
+    }
+  }
+}
+
+// ------------------------------------------------------------------ launchers
+template <typename T, int D, bool CAP, bool BIAS>
+static hipError_t launch_scored_bwd_kernels(const ScoredBwdParams& p, hipStream_t stream) {
+  using K = ScoredKvTile<T, D>;
+  using Q = ScoredDqTile<T, D>;
+  ScoredBwdParams a = p;
+  void* args[] = {&a};
+  a.n_ktiles = (int)((p.n_k + K::BKG - 1) / K::BKG);
+  a.n_qtiles = (int)((p.n_q + Q::ROWS - 1) / Q::ROWS);
+  const int bias = bias_lds_bytes(p.s, 1);
+  hipError_t e = hipSuccess;
+  if (p.dk) {
+    e = hipLaunchKernel(reinterpret_cast<const void*>(scored_dkdv_kernel<T, D, CAP, BIAS>),
+                        dim3((unsigned)((int64_t)a.n_ktiles * p.n_b * p.heads_kv)), dim3(K::NT), args, K::LDS_BYTES + bias,
+                        stream);
+    if (e != hipSuccess) return e;
+  }
+  if (!p.dq) return e;
+  const int bins = p.table_part ? 8 * bias_places(p.s) * 4 : 0;
+  e = hipLaunchKernel(reinterpret_cast<const void*>(scored_dq_kernel<T, D, CAP, BIAS>),
+                      dim3((unsigned)((int64_t)a.n_qtiles * p.n_b * p.s.heads)), dim3(Q::NT), args,
+                      Q::LDS_BYTES + bias + bins, stream);
+  if (e != hipSuccess || !p.table_part) return e;
+  return launch_scored_table(a, stream);
+}
+template <typename T, int D>
+static hipError_t launch_scored_bwd_d(const ScoredBwdParams& p, hipStream_t stream) {
+  ScoredBwdParams a = p;
+  void* args[] = {&a};
+  constexpr int RPB = 256 / (D * (int)sizeof(T) / 16);
+  const int64_t rows = (int64_t)p.n_b * p.s.heads * p.n_q_pad;
+  const hipError_t e = hipLaunchKernel(reinterpret_cast<const void*>(scored_bwd_pre_kernel<T, D>),
+                                       dim3((unsigned)((rows + RPB - 1) / RPB)), dim3(256), args, 0, stream);
+  if (e != hipSuccess) return e;
+  const bool cap = p.s.cap2 != 0.0f, bias = p.s.slopes || p.s.table;
+  if (cap)
+    return bias ? launch_scored_bwd_kernels<T, D, true, true>(p, stream)
+                : launch_scored_bwd_kernels<T, D, true, false>(p, stream);
+  return bias ? launch_scored_bwd_kernels<T, D, false, true>(p, stream)
+              : launch_scored_bwd_kernels<T, D, false, false>(p, stream);
+}
+template <typename T>
+hipError_t launch_scored_bwd(const ScoredBwdParams& p, int d, hipStream_t stream) {
+  return d == 64 ? launch_scored_bwd_d<T, 64>(p, stream) : launch_scored_bwd_d<T, 128>(p, stream);
+}
+
+}  // namespace mea

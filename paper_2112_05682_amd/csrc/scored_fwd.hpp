@@ -1,0 +1,552 @@
+// The stream kernel: rows of queries against keys with the lazy softmax
+// (arXiv 2112.05682, Sections 2-4) of modified scores (scored.hpp).
+//
+// A workgroup is 4 waves.  RW of them own 32 rows each, and with RW < 4 the
+// others take shares of the same rows' keys (KW = 4 / RW), whose summaries are
+// combined in LDS.  S^T = K Q^T puts a row on each lane, so that a row's limit,
+// position, document, slope and softmax state are scalars of the lane.  16-bit
+// K and V tiles go to LDS by asynchronous copies into swizzled rows, two stages;
+// with RW = 1 a wave copies the keys it reads, so that the waves run without a
+// barrier.  float32 tiles are split into their three parts on the way.
+#pragma once
+
+#include "scored.hpp"
+
+namespace mea {
+
+template <typename T, int D, int RW>
+struct StreamTile {
+  static constexpr bool F32 = sizeof(T) == 4;
+  static constexpr int NT = 256, KW = 4 / RW, ROWS = 32 * RW;
+  static constexpr int BK = stream_tile(!F32, RW), BKW = BK / KW;
+  static constexpr int NP = Planes<T>::NP;
+  // float32: padded rows of three bf16 planes (the pads as in FwdTile).
+  static constexpr int RSK = D + 8, RSV = D + 32;
+  static constexpr int TILEK = BK * RSK, TILEV = BK * RSV;
+  static constexpr int STAGE_BYTES = F32 ? NP * (TILEK + TILEV) * 2 : 2 * BK * D * 2;
+  // Workgroups per CU that the registers are kept to.
+  static constexpr int OCC = F32 ? (D == 64 && RW == 4 ? 2 : 1) : (RW == 1 ? (D == 64 ? 2 : 1) : (D == 64 ? 3 : 2));
+  static constexpr int kBiasMax = 4 * (2 * kMaxBiasSpan + 1) + 16;
+  static constexpr int NBUF = 2 * STAGE_BYTES + kBiasMax <= 160 * 1024 / OCC ? 2 : 1;
+  static constexpr int ML_BYTES = 2 * 4 * 32 * 4;
+  static constexpr int RED_BYTES = KW > 1 ? ML_BYTES + RW * (D / 32) * (KW - 1) * 4096 : 0;
+  static constexpr int LDS_BYTES = NBUF * STAGE_BYTES > RED_BYTES ? NBUF * STAGE_BYTES : RED_BYTES;
+  // Chunks a thread stages (float32).
+  static constexpr int CPR = D / 8, CHUNKS = 2 * BK * CPR, CPT = CHUNKS / NT;
+  static_assert(CHUNKS % NT == 0 && BKW % 32 == 0, "tile shapes");
+  static_assert(F32 || NBUF == 2, "asynchronous copies need two stages");
+  static_assert((LDS_BYTES + kBiasMax) * OCC <= 160 * 1024, "LDS");
+};
+
+template <typename T, int D, int RW, bool CAP, bool BIAS>
+__global__ __launch_bounds__(256, (StreamTile<T, D, RW>::OCC)) void scored_stream_kernel(StreamParams p) {
+  using C = StreamTile<T, D, RW>;
+  using LE = typename Planes<T>::E;
+  constexpr bool F32 = C::F32;
+  constexpr int KW = C::KW, BK = C::BK, BKW = C::BKW, KC = D / 16, NKT = BKW / 32, NPC = BKW / 16, NDT = D / 32;
+  // Whether scores hold 2^s exponents (else raw products, times scale log2 e later).
+  constexpr bool LOG2 = CAP || BIAS;
+
+  extern __shared__ __align__(16) unsigned char smem[];
+  unsigned char* const lds_bias = smem + C::LDS_BYTES;
+  __shared__ int4 wave_ids[4];
+
+  const ScoreArgs& sa = p.s;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+  const int h = lane >> 5, c = lane & 31;
+  const int wave_q = RW == 4 ? wave : wave % RW, wave_k = RW == 4 ? 0 : wave / RW;
+
+  // ---- workgroup -> row tile, group, key range.
+  const TileItem item = tile_item(blockIdx.x, gridDim.x, p.n_rtiles, p.tile_order);
+  const int rtile = sa.causal ? p.n_rtiles - 1 - item.tile : item.tile;  // longest rows first
+  const int split = item.group / p.n_groups;
+  int gi = item.group % p.n_groups;
+  const int sub = gi % p.groups_per_kv;
+  gi /= p.groups_per_kv;
+  const int b0 = gi % p.n_b, kvh = gi / p.n_b;
+  const int head0 = kvh * p.heads_per_kv + sub * p.fold;
+
+  // ---- this lane's row.
+  const int64_t row0 = (int64_t)rtile * C::ROWS;
+  const int64_t row_last = (row0 + C::ROWS < p.group_rows ? row0 + C::ROWS : p.group_rows) - 1;
+  const int64_t row = row0 + 32 * wave_q + c;
+  const bool in_rows = row < p.group_rows;
+  const int64_t rr = in_rows ? row : row_last;
+  const int g = (int)(rr % p.fold);
+  const int64_t x = rr / p.fold;
+  const int64_t qi = x % p.n_q;
+  const int b = b0 + (int)(x / p.n_q);
+  const int head = head0 + g;
+
+  const int64_t n_kv = batch_keys(sa, b0, p.n_k);
+  const int64_t pos0 = first_pos(sa, b0);
+  int64_t lim = in_rows ? key_limit(sa, b0, n_kv, pos0 + qi) : 0;
+  // Limits grow with the query, so the tile's first and last rows bound them (a
+  // group of several batches has no positional mask).
+  const int64_t lim_hi = key_limit(sa, b0, n_kv, pos0 + (row_last / p.fold) % p.n_q);
+  const int64_t lim_lo = key_limit(sa, b0, n_kv, pos0 + (row0 / p.fold) % p.n_q);
+  const int64_t w_row0 = row0 + 32 * wave_q;
+  const int64_t w_last = w_row0 + 31 < p.group_rows ? w_row0 + 31 : p.group_rows - 1;
+  // The wave's first and last query (uniform), and its limit.
+  const bool wave_rows = w_row0 < p.group_rows;
+  const int64_t wq_lo = pos0 + w_row0 / p.fold % p.n_q, wq_hi = pos0 + (wave_rows ? w_last / p.fold % p.n_q : 0);
+  const int64_t w_lim = wave_rows ? key_limit(sa, b0, n_kv, wq_hi) : 0;
+
+  int doc = -2;
+  int4 ids = make_int4(0, 0, 0, 0);
+  if (sa.q_doc) {
+    if (in_rows) doc = sa.q_doc[(int64_t)b * p.n_q + qi];
+    if (doc < 0) {
+      doc = -2;
+      lim = 0;
+    }
+    ids = workgroup_ids(doc, wave, lane, wave_ids);
+  }
+  constexpr int UNITS = BK / 32;
+  const int n_units = (int)((p.n_k + 31) / 32);
+  DocTiles<UNITS> docs(sa.k_range ? sa.k_range + (int64_t)b0 * n_units : nullptr, n_units, ids.x, ids.y);
+
+  const float slope2 = BIAS && sa.slopes ? sa.slopes[head] * kLog2eF : 0.0f;
+  if (BIAS && sa.table) fill_bias(sa, lds_bias, p.fold, head0, tid, C::NT);
+
+  // ---- keys of this range: the visible tiles dealt evenly.
+  const int all_tiles = (int)((lim_hi + BK - 1) / BK);
+  const int per = (all_tiles + p.n_splits - 1) / p.n_splits;
+  const int t0 = split * per;
+  const int t1 = t0 + per < all_tiles ? t0 + per : all_tiles;
+  const int64_t kb = p.batches > 1 ? 0 : (int64_t)b0;
+  const T* __restrict__ kg = static_cast<const T*>(p.k) + kb * p.sk.b + (int64_t)kvh * p.sk.h;
+  const T* __restrict__ vg = static_cast<const T*>(p.v) + kb * p.sv.b + (int64_t)kvh * p.sv.h;
+
+  // ---- Q^T as B operands: lane (h, row c) holds features 16 kc + 8 h ..
+  Range<T, false> range;
+  Frag<T> qf[KC];
+  {
+    const T* qg = static_cast<const T*>(p.q) + (int64_t)b * p.sq.b + (int64_t)head * p.sq.h + qi * p.sq.r;
+#pragma unroll
+    for (int kc = 0; kc < KC; ++kc)
+      qf[kc] = lim > 0 ? ld_frag_as<T, T>(qg + 16 * kc + 8 * h, range) : zero_frag<T>();
+  }
+
+  f32x16 acc[NDT];
+#pragma unroll
+  for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) acc[dt][r] = 0.0f;
+  float m_ref = -INFINITY, l_run = 0.0f;
+  wait_global_loads();
+  __syncthreads();  // the bias is there
+
+  // ---- staging.  16-bit: copies of 1 KiB, rows past the last visible key repeat
+  // it (finite, and masked); with RW = 1 each wave copies its own keys.
+  constexpr int CPR = C::CPR, RPU = 64 / CPR;
+  constexpr bool OWN = RW == 1;
+  constexpr int UNITS_K = BK / RPU, UPW = UNITS_K / 4;  // copies of K (and of V) per tile and wave
+  const int urow = lane / CPR, uch = lane % CPR;
+  auto copy_tile = [&](int t, int buf) __attribute__((always_inline)) {
+    const int64_t k0 = (int64_t)t * BK;
+    const unsigned base = __builtin_amdgcn_readfirstlane(lds_addr(smem + buf * C::STAGE_BYTES));
+#pragma unroll
+    for (int j = 0; j < UPW; ++j) {
+      const int u = OWN ? wave * UPW + j : wave + 4 * j;
+      const int r = RPU * u + urow;
+      int64_t key = k0 + r;
+      if (key > lim_hi - 1) key = lim_hi - 1;
+      const int ch = 8 * (uch ^ swz<D>(r));
+      copy_to_lds16<OWN>(kg + key * p.sk.r + ch, base + 1024u * (unsigned)u);
+      copy_to_lds16<OWN>(vg + key * p.sv.r + ch, base + (unsigned)(BK * D * 2) + 1024u * (unsigned)u);
+    }
+  };
+  Chunk8<T> stage[F32 ? C::CPT : 1];
+  auto load_stage = [&](int t) __attribute__((always_inline)) {
+    if constexpr (F32) {
+#pragma unroll
+      for (int i = 0; i < C::CPT; ++i) {
+        const int chunk = tid + i * C::NT;
+        const bool is_v = chunk >= BK * CPR;
+        const int rem = is_v ? chunk - BK * CPR : chunk;
+        const int r = rem / CPR, col = rem % CPR;
+        const int64_t key = (int64_t)t * BK + r;
+        const T* src = is_v ? vg + key * p.sv.r : kg + key * p.sk.r;
+        stage[i] = key < lim_hi ? ld_chunk8<T, T>(src + 8 * col) : zero_chunk8<T>();
+      }
+    }
+  };
+  auto store_stage = [&](int buf) __attribute__((always_inline)) {
+    if constexpr (F32) {
+      LE* base = reinterpret_cast<LE*>(smem + buf * C::STAGE_BYTES);
+#pragma unroll
+      for (int i = 0; i < C::CPT; ++i) {
+        const int chunk = tid + i * C::NT;
+        const bool is_v = chunk >= BK * CPR;
+        const int rem = is_v ? chunk - BK * CPR : chunk;
+        const int r = rem / CPR, col = rem % CPR;
+        st_chunk8<T>(base + (is_v ? C::NP * C::TILEK + r * C::RSV : r * C::RSK) + 8 * col, is_v ? C::TILEV : C::TILEK,
+                     stage[i], range);
+      }
+    }
+  };
+
+  const int krow = perm32(c);
+  const float cl2 = p.scale_log2;
+
+  auto tile = [&](auto mask_tag, int t, int buf, bool one_doc) {
+    constexpr bool MASK = decltype(mask_tag)::value;
+    const int64_t k0 = (int64_t)t * BK + BKW * wave_k;
+    if (k0 >= w_lim) return;  // all keys beyond this wave's rows
+    const unsigned char* st = smem + buf * C::STAGE_BYTES;
+    const LE* ks = reinterpret_cast<const LE*>(st) + BKW * wave_k * C::RSK;             // float32
+    const LE* vs = reinterpret_cast<const LE*>(st) + C::NP * C::TILEK + BKW * wave_k * C::RSV;
+    const unsigned char* kt16 = st + BKW * wave_k * (2 * D);                            // 16-bit
+    const unsigned char* vt16 = st + BK * D * 2 + BKW * wave_k * (2 * D);
+
+    f32x16 s[NKT];
+#pragma unroll
+    for (int kt = 0; kt < NKT; ++kt)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[kt][r] = 0.0f;
+    f32x16 rest[F32 ? NKT : 1] = {};
+#pragma unroll
+    for (int kc = 0; kc < KC; ++kc)
+#pragma unroll
+      for (int kt = 0; kt < NKT; ++kt) {
+        if constexpr (F32) {
+          const Frag<T> a = lds_frag_planes<T>(ks + (32 * kt + krow) * C::RSK + 16 * kc + 8 * h, C::TILEK);
+          rest[kt] = mma_rest(a, qf[kc], rest[kt]);
+          s[kt] = mma(lead(a), lead(qf[kc]), s[kt]);
+        } else {
+          s[kt] = mma(row_frag<T, D>(kt16, 32 * kt + krow, 2 * kc + h), qf[kc], s[kt]);
+        }
+      }
+    if constexpr (F32)
+#pragma unroll
+      for (int kt = 0; kt < NKT; ++kt) s[kt] += rest[kt];
+
+    // Cap and bias.
+    if constexpr (LOG2) {
+#pragma unroll
+      for (int kt = 0; kt < NKT; ++kt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[kt][r] = CAP ? sa.cap2 * cap_tanh<T>(sa, s[kt][r]) : s[kt][r] * cl2;
+    }
+    if constexpr (BIAS) {
+      const int off = rel(k0 - (pos0 + qi));  // first key's distance
+      if (sa.slopes) {
+        const float d0 = (float)off;
+#pragma unroll
+        for (int kt = 0; kt < NKT; ++kt)
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            s[kt][r] = fmaf(-fabsf(d0 + (float)(32 * kt + permuted_row(r, h))), slope2, s[kt][r]);
+      }
+      if (sa.table) {
+        const int hi = sa.two_sided ? sa.span : 0, last = bias_places(sa) - 1;
+#pragma unroll
+        for (int kt = 0; kt < NKT; ++kt) {
+          const int64_t ka = k0 + 32 * kt;
+          if (ka + 31 <= wq_lo - sa.span || ka >= wq_hi + hi) {  // one value for every key of a row
+            const float v = bias_at(sa, lds_bias, p.fold, g, ka >= wq_hi + hi ? last : 0);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[kt][r] += v;
+          } else {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+              int d = off + 32 * kt + permuted_row(r, h);
+              d = d < -sa.span ? -sa.span : (d > hi ? hi : d);
+              s[kt][r] += bias_at(sa, lds_bias, p.fold, g, d + sa.span);
+            }
+          }
+        }
+      }
+    }
+
+    // Masks.  absent: bit e of byte pc, key 16 pc + 8 h + e has no document.
+    uint32_t absent = 0;
+    static_assert(NPC <= 4, "a byte for each 16 keys");
+    if constexpr (MASK) {
+      const int l = rel(lim - k0);
+#pragma unroll
+      for (int kt = 0; kt < NKT; ++kt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (32 * kt + permuted_row(r, h) >= l) s[kt][r] = -INFINITY;
+      if (sa.q_doc && !one_doc) {
+#pragma unroll
+        for (int kt = 0; kt < NKT; ++kt) {
+          const int64_t key = k0 + 32 * kt + c;
+          const int mine = key < p.n_k ? sa.k_doc[(int64_t)b0 * p.n_k + key] : -1;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int id = __shfl(mine, permuted_row(r, h));
+            if (id != doc) s[kt][r] = -INFINITY;
+            if (id < 0) absent |= 1u << (8 * (2 * kt + r / 8) + r % 8);
+          }
+        }
+      }
+    }
+
+    // Lazy softmax, one row per lane (both halves hold keys of the same row).
+    float mx = -INFINITY;
+#pragma unroll
+    for (int kt = 0; kt < NKT; ++kt)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[kt][r]);
+    const float mul = LOG2 ? 1.0f : cl2;
+    const float mx_c = xhalf_max(mx) * mul;
+    const bool raise = mx_c > m_ref + kRescaleSlack;
+    if (__builtin_amdgcn_ballot_w64(raise)) {
+      const float m_new = raise ? mx_c : m_ref;
+      const float alpha = raise ? fast_exp2(m_ref - m_new) : 1.0f;
+      l_run *= alpha;
+#pragma unroll
+      for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[dt][r] *= alpha;
+      m_ref = m_new;
+    }
+    const float neg = (MASK && m_ref == -INFINITY) ? 0.0f : -m_ref;
+    Frag<T> pf[NPC];
+#pragma unroll
+    for (int pc = 0; pc < NPC; ++pc) {
+      float e8[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float v = s[pc >> 1][8 * (pc & 1) + e];
+        e8[e] = fast_exp2(LOG2 ? v + neg : fmaf(v, cl2, neg));
+      }
+      pf[pc] = to_frag<T>(e8);
+      l_run = tree_sum<8>(e8, l_run);
+    }
+    // O^T += V^T P^T; keys without a document are taken out of V, whatever they hold.
+    const bool drop = MASK && __builtin_amdgcn_ballot_w64(absent != 0);
+#pragma unroll
+    for (int dt = 0; dt < NDT; ++dt) {
+      f32x16 sum = {};
+#pragma unroll
+      for (int pc = 0; pc < NPC; ++pc) {
+        Frag<T> a;
+        if constexpr (F32) a = lds_col_frag_planes<T>(vs, C::TILEV, C::RSV, 16 * pc, 32 * dt, lane);
+        else a = col_frag<T, D>(vt16, 16 * pc, 32 * dt, lane);
+        if constexpr (MASK)
+          if (drop) a = without<T>(a, absent >> (8 * pc));
+        if constexpr (F32) sum = mma(a, pf[pc], sum);
+        else acc[dt] = mma(a, pf[pc], acc[dt]);
+      }
+      if constexpr (F32) acc[dt] += sum;  // a tile's products are added once
+    }
+  };
+
+  // ---- the loop over the visible tiles of this range.
+  int t = docs.next(t0, t1), buf = 0;
+  if constexpr (F32) {
+    if (t < t1) {
+      load_stage(t);
+      store_stage(0);
+    }
+    __syncthreads();
+  } else {
+    if (t < t1) copy_tile(t, 0);
+  }
+  while (t < t1) {
+    const int tn = docs.next(t + 1, t1);
+    const bool one_doc = ids.z == 0 && docs.uniform(t);
+    const bool plain = (int64_t)(t + 1) * BK <= lim_lo && one_doc && row_last - row0 == C::ROWS - 1;
+    if constexpr (F32) {
+      if (tn < t1) load_stage(tn);
+    } else {
+      wait_global_loads();
+      if constexpr (!OWN) __syncthreads();
+      else wait_lds_reads();
+      if (tn < t1) copy_tile(tn, buf ^ 1);
+    }
+    if (plain) tile(std::false_type{}, t, buf, true);
+    else tile(std::true_type{}, t, buf, one_doc);
+    if constexpr (F32) {
+      if (C::NBUF == 1) __syncthreads();
+      if (tn < t1) store_stage(C::NBUF == 1 ? 0 : buf ^ 1);
+      __syncthreads();
+    }
+    if (C::NBUF == 2) buf ^= 1;
+    t = tn;
+  }
+
+  // ---- KW > 1: one summary of the waves that share the rows, in their order.
+  float l_sum = xhalf_sum(l_run);
+  if constexpr (KW > 1) {
+    __syncthreads();  // every wave is done with the stages
+    float* red_m = reinterpret_cast<float*>(smem);
+    float* red_l = red_m + 128;
+    float* red_o = red_m + C::ML_BYTES / 4 + wave_q * NDT * (KW - 1) * 1024 + lane;
+    if (h == 0) {
+      red_m[wave * 32 + c] = m_ref;
+      red_l[wave * 32 + c] = l_sum;
+    }
+    __syncthreads();
+    float m_g = -INFINITY, l_g = 0.0f;
+#pragma unroll
+    for (int y = 0; y < KW; ++y) m_g = fmaxf(m_g, red_m[(wave_q + y * RW) * 32 + c]);
+#pragma unroll
+    for (int y = 0; y < KW; ++y) {
+      const float m_y = red_m[(wave_q + y * RW) * 32 + c];
+      l_g += (m_y == -INFINITY ? 0.0f : fast_exp2(m_y - m_g)) * red_l[(wave_q + y * RW) * 32 + c];
+    }
+    const float f = m_ref == -INFINITY ? 0.0f : fast_exp2(m_ref - m_g);
+    m_ref = m_g;
+    l_sum = l_g;
+#pragma unroll
+    for (int dt = 0; dt < NDT; ++dt) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[dt][r] *= f;
+      if (dt % KW != wave_k)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) red_o[((dt * (KW - 1) + wave_k - (wave_k > dt % KW)) * 16 + r) * 64] = acc[dt][r];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int dt = 0; dt < NDT; ++dt)
+      if (dt % KW == wave_k)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+#pragma unroll
+          for (int y = 0; y < KW - 1; ++y) acc[dt][r] += red_o[((dt * (KW - 1) + y) * 16 + r) * 64];
+  }
+
+  // ---- epilogue.
+  if (!in_rows) return;
+  const int64_t out_row = ((int64_t)b * sa.heads + head) * p.n_q + qi;
+  if (p.direct) {
+    const float inv = l_sum == 0.0f ? 0.0f : 1.0f / l_sum;  // no visible key: o = 0
+    T* og = static_cast<T*>(p.o) + (int64_t)b * p.so.b + (int64_t)head * p.so.h + qi * p.so.r;
+    T* gl = p.o_lo ? static_cast<T*>(p.o_lo) + out_row * D : nullptr;
+#pragma unroll
+    for (int dt = 0; dt < NDT; ++dt) {
+      if (KW > 1 && dt % KW != wave_k) continue;
+#pragma unroll
+      for (int a4 = 0; a4 < 4; ++a4) {
+        float x4[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x4[e] = acc[dt][4 * a4 + e] * inv;
+        const int f = 32 * dt + 8 * a4 + 4 * h;
+        store_out4<T>(og + f, gl ? gl + f : nullptr, x4);
+      }
+    }
+    if (h == 0 && wave_k == 0 && p.lse) p.lse[out_row] = l_sum == 0.0f ? -INFINITY : (m_ref + __log2f(l_sum)) * kLn2F;
+  } else {
+    const int64_t prow = (int64_t)(p.split0 + split) * p.out_rows + out_row;
+    float* po = p.part_o + prow * D;
+#pragma unroll
+    for (int dt = 0; dt < NDT; ++dt) {
+      if (KW > 1 && dt % KW != wave_k) continue;
+#pragma unroll
+      for (int a4 = 0; a4 < 4; ++a4) {
+        f32x4 v4;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v4[e] = acc[dt][4 * a4 + e];
+        *reinterpret_cast<f32x4*>(po + 32 * dt + 8 * a4 + 4 * h) = v4;
+      }
+    }
+    if (h == 0 && wave_k == 0) {
+      p.part_m[prow] = m_ref;
+      p.part_l[prow] = l_sum;
+    }
+  }
+}
+
+// Combine of the summaries of n_parts key ranges (Section 4): rescaled to the
+// common maximum, added, divided.  A thread per row and 4 features.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void scored_combine_kernel(StreamParams p, int n_parts) {
+  constexpr int G4 = D / 4;
+  const int64_t gid = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (gid >= p.out_rows * G4) return;
+  const int64_t row = gid / G4;
+  const int f0 = 4 * (int)(gid % G4);
+  float m = -INFINITY, l = 0.0f;
+  f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+  // Eight ranges at a time, their loads in flight together.
+  for (int s0 = 0; s0 < n_parts; s0 += 8) {
+    float ms[8], ls[8];
+    f32x4 os[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const bool in = s0 + i < n_parts;
+      const int64_t at = (int64_t)(in ? s0 + i : s0) * p.out_rows + row;
+      ms[i] = p.part_m[at];
+      ls[i] = p.part_l[at];
+      os[i] = *reinterpret_cast<const f32x4*>(p.part_o + at * D + f0);
+      if (!in) ms[i] = -INFINITY;
+    }
+    float mx = m;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) mx = fmaxf(mx, ms[i]);
+    const float a = m == -INFINITY ? 0.0f : fast_exp2(m - mx);
+    l *= a;
+    o *= a;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      // (0 times a NaN denominator, a range of NaN scores only, stays NaN)
+      const float w = ms[i] == -INFINITY ? 0.0f : fast_exp2(ms[i] - mx);
+      l = fmaf(w, ls[i], l);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] = fmaf(w, os[i][e], o[e]);
+    }
+    m = mx;
+  }
+  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+  float x4[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) x4[e] = o[e] * inv;
+  const int64_t qi = row % p.n_q, bh = row / p.n_q;
+  T* og = static_cast<T*>(p.o) + bh / p.s.heads * p.so.b + bh % p.s.heads * p.so.h + qi * p.so.r;
+  T* gl = p.o_lo ? static_cast<T*>(p.o_lo) + row * D : nullptr;
+  store_out4<T>(og + f0, gl ? gl + f0 : nullptr, x4);
+  if (f0 == 0 && p.lse) p.lse[row] = l == 0.0f ? -INFINITY : (m + __log2f(l)) * kLn2F;
+}
+
+// ------------------------------------------------------------------ launchers
+template <typename T, int D, int RW, bool CAP, bool BIAS>
+static hipError_t launch_stream_kernel(const StreamParams& p, hipStream_t stream) {
+  using C = StreamTile<T, D, RW>;
+  StreamParams q = p;
+  q.n_rtiles = (int)((p.group_rows + C::ROWS - 1) / C::ROWS);
+  const int lds = C::LDS_BYTES + bias_lds_bytes(p.s, p.fold);
+  const int64_t grid = (int64_t)q.n_rtiles * p.n_groups * p.n_splits;
+  if (grid < 1 || grid >= ((int64_t)1 << 31) || lds > 160 * 1024 - 64) return hipErrorInvalidValue;
+  void* args[] = {&q};
+  return hipLaunchKernel(reinterpret_cast<const void*>(scored_stream_kernel<T, D, RW, CAP, BIAS>), dim3((unsigned)grid),
+                         dim3(C::NT), args, lds, stream);
+}
+template <typename T, int D, int RW>
+static hipError_t launch_stream_mods(const StreamParams& p, hipStream_t stream) {
+  const bool cap = p.s.cap2 != 0.0f, bias = p.s.slopes || p.s.table;
+  if (cap)
+    return bias ? launch_stream_kernel<T, D, RW, true, true>(p, stream)
+                : launch_stream_kernel<T, D, RW, true, false>(p, stream);
+  return bias ? launch_stream_kernel<T, D, RW, false, true>(p, stream)
+              : launch_stream_kernel<T, D, RW, false, false>(p, stream);
+}
+template <typename T, int D>
+static hipError_t launch_stream_rows(const StreamParams& p, int row_waves, hipStream_t stream) {
+  switch (row_waves) {
+    case 4: return launch_stream_mods<T, D, 4>(p, stream);
+    case 2: return launch_stream_mods<T, D, 2>(p, stream);
+    case 1:
+      if constexpr (sizeof(T) == 2) return launch_stream_mods<T, D, 1>(p, stream);
+  }
+  return hipErrorInvalidValue;
+}
+template <typename T>
+hipError_t launch_stream(const StreamParams& p, int d, int row_waves, hipStream_t stream) {
+  return d == 64 ? launch_stream_rows<T, 64>(p, row_waves, stream) : launch_stream_rows<T, 128>(p, row_waves, stream);
+}
+template <typename T>
+hipError_t launch_scored_combine(const StreamParams& p, int d, int n_parts, hipStream_t stream) {
+  StreamParams q = p;
+  void* args[] = {&q, &n_parts};
+  const int64_t threads = p.out_rows * (d / 4);
+  const void* k = d == 64 ? reinterpret_cast<const void*>(scored_combine_kernel<T, 64>)
+                          : reinterpret_cast<const void*>(scored_combine_kernel<T, 128>);
+  return hipLaunchKernel(k, dim3((unsigned)((threads + 255) / 256)), dim3(256), args, 0, stream);
+}
+
+}  // namespace mea

@@ -1,0 +1,76 @@
+"""Attention of a batch that shares a prefix against float64 attention over the prefix's
+and the own keys in a row."""
+import pytest
+import torch
+
+from paper_2112_05682_amd import attention_shared_prefix
+from scored_ref import assert_within, reference
+
+pytestmark = pytest.mark.gpu
+
+DT = {"fp32": torch.float32, "fp16": torch.float16, "bf16": torch.bfloat16}
+
+CASES = [  # dtype, B, H, Hkv, nq, n_p, n_k, d, causal, kv_len
+    ("bf16", 3, 8, 2, 1, 1000, 40, 128, False, [40, 1, 0]),
+    ("fp16", 5, 4, 4, 4, 333, 77, 64, True, [77, 4, 30, 9, 60]),
+    ("fp32", 2, 4, 2, 1, 500, 20, 64, False, [20, 3]),
+    ("fp32", 3, 2, 1, 3, 64, 65, 128, True, [65, 3, 33]),
+    ("bf16", 40, 6, 2, 1, 2500, 200, 64, False, None),
+    ("bf16", 1, 2, 2, 1, 1, 1, 64, False, None),
+    ("fp16", 1, 3, 1, 100, 200, 100, 128, True, None),
+    ("bf16", 70, 8, 1, 1, 129, 33, 128, False, None),
+    ("bf16", 20, 16, 16, 8, 100, 9, 64, True, None),
+]
+
+
+def make(case, seed=0):
+    dtype, B, H, Hkv, nq, n_p, nk, d, causal, lens = case
+    g = torch.Generator().manual_seed(seed)
+    shapes = ((B, H, nq, d), (Hkv, n_p, d), (Hkv, n_p, d), (B, Hkv, nk, d), (B, Hkv, nk, d))
+    return [(torch.randn(s, generator=g) * (2.0 if i == 0 else 1.0)).to(DT[dtype]) for i, s in enumerate(shapes)]
+
+
+def expected(case, q, kp, vp, k, v):
+    """The own keys follow the prefix: positions and lengths are moved by n_p."""
+    dtype, B, H, Hkv, nq, n_p, nk, d, causal, lens = case
+    lens = [nk] * B if lens is None else lens
+    both = [torch.cat([t[None].expand(B, -1, -1, -1), own], 2) for t, own in ((kp, k), (vp, v))]
+    pos = [n - nq + n_p for n in lens] if causal else None
+    return reference(q, *both, dtype=DT[dtype], causal=causal, q_pos=pos, prefix_len=[n_p] * B if causal else None,
+                     kv_len=[n + n_p for n in lens])
+
+
+@pytest.mark.parametrize("case", CASES, ids=lambda c: "-".join(map(str, c[:9])))
+def test_shared_prefix(case):
+    dtype, B, H, Hkv, nq, n_p, nk, d, causal, lens = case
+    print("prefix", case[:9], flush=True)
+    x = make(case)
+    if lens is not None:  # garbage behind the own keys
+        for b, n in enumerate(lens):
+            x[3][b, :, n:], x[4][b, :, n:] = float("nan"), float("nan")
+    ref = expected(case, *x)
+    kl = None if lens is None else torch.tensor(lens, dtype=torch.int32, device="cuda")
+    pos = torch.tensor([n - nq for n in (lens or [nk] * B)], dtype=torch.int32, device="cuda") if causal else None
+    o, lse = attention_shared_prefix(*(t.cuda() for t in x), causal=causal, kv_len=kl, q_pos=pos, need_lse=True)
+    torch.cuda.synchronize()
+    assert_within("o", o, ref["o"])
+    assert_within("lse", lse, ref["lse"])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_strides(dtype):
+    """Token-major caches, the prefix a slice of one sequence's cache."""
+    B, H, Hkv, nq, n_p, nk, d = 3, 4, 2, 2, 150, 50, 64
+    g = torch.Generator().manual_seed(2)
+    mk = lambda *s: torch.randn(s, generator=g).to(DT[dtype])  # noqa: E731
+    q, k, v = mk(B, nq, H, d).transpose(1, 2), mk(B, nk, Hkv, d).transpose(1, 2), mk(B, nk, Hkv, d).transpose(1, 2)
+    cache_k, cache_v = mk(B, 400, Hkv, d), mk(B, 400, Hkv, d)
+    kp, vp = (t[1, 30:30 + n_p].transpose(0, 1) for t in (cache_k, cache_v))
+    case = (dtype, B, H, Hkv, nq, n_p, nk, d, False, None)
+    ref = expected(case, q, kp, vp, k, v)
+    dev = [t.cuda() for t in (q, k, v)]
+    kg, vg = (t.cuda()[1, 30:30 + n_p].transpose(0, 1) for t in (cache_k, cache_v))
+    out = torch.empty(B, nq, H, d, dtype=DT[dtype], device="cuda").transpose(1, 2)
+    assert attention_shared_prefix(dev[0], kg, vg, dev[1], dev[2], out=out) is out
+    torch.cuda.synchronize()
+    assert_within("o", out, ref["o"])
