@@ -77,6 +77,14 @@ struct StreamParams {
   int direct;          // 1: one range, o and lse are written; 0: summaries
   int tile_order;
   float scale_log2;
+  // The reference maximum is raised by a score that exceeds it by more than this
+  // many powers of two: kRescaleSlack where only o is wanted, 0 where a backward will
+  // follow.  A row's largest weight is then exactly 1 when it is rounded to 16 bits, and
+  // D_i = dO_i . o_i, which that row's dS is a small difference from, is not off by its
+  // rounding (scores of standard deviation 4, causal 2048 keys, in float64 with these
+  // roundings: dS off by 5e-4 of itself, 2.1e-3 with weights up to 2^8; dQ 2.46e-3 and
+  // 3.28e-3, of which 2.40e-3 are the roundings of dS and of dQ itself).
+  float slack;
   TensorStrides sq, sk, sv, so;
   ScoreArgs s;
 };
@@ -108,6 +116,60 @@ __device__ __forceinline__ Frag<T> col_frag(const unsigned char* tile, int row0,
   r8[4] = hi[0]; r8[5] = hi[1]; r8[6] = hi[2]; r8[7] = hi[3];
   return __builtin_bit_cast(Frag<T>, r8);
 }
+
+// Asynchronous copies of ROWS rows of two 16-bit tensors into swizzled LDS tiles,
+// by 4 waves, 1 KiB (64 / CPR rows) an instruction.  A whole tile's copies take one
+// byte offset per lane and tensor, computed once, and scalar bases: wave w copies
+// units w, w + 4, .., rows that share their swizzle.  OWN: a wave copies its quarter
+// of the rows (which it alone reads), whose swizzle repeats every 16 rows.  Rows from
+// `end` on repeat the last one before it.
+template <typename T, int D, int ROWS, bool OWN>
+struct TileCopy {
+  static constexpr int CPR = D / 8, RPU = 64 / CPR, UPW = ROWS / RPU / 4;
+  static constexpr int NV = OWN ? 16 / RPU : 1;  // offsets
+  static constexpr int STEP = OWN ? 16 : 4 * RPU;  // rows between units of one offset
+  static_assert(UPW % NV == 0 && (OWN || 4 * RPU % 16 == 0), "swizzle period");
+  unsigned va[NV], vb[NV];
+  int first, lane_chunk;  // this lane's first row, and its physical chunk
+  __device__ __forceinline__ TileCopy(int wave, int lane, int64_t row_a, int64_t row_b) {
+    first = (OWN ? wave * (ROWS / 4) : wave * RPU) + lane / CPR;
+    lane_chunk = lane % CPR;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int r = lane / CPR + RPU * i;  // from the wave's first row
+      const unsigned ch = 16u * (unsigned)(lane_chunk ^ swz<D>(first + RPU * i));
+      va[i] = 2u * (unsigned)r * (unsigned)row_a + ch;
+      vb[i] = 2u * (unsigned)r * (unsigned)row_b + ch;
+    }
+  }
+  __device__ __forceinline__ void operator()(const T* a, int64_t row_a, const T* b, int64_t row_b, int64_t r0, int64_t end,
+                                             unsigned lds, int wave) const {
+    const int w0 = OWN ? wave * (ROWS / 4) : wave * RPU;  // uniform
+    const unsigned dst = lds + (unsigned)(w0 * 2 * D);
+    constexpr unsigned TILE = ROWS * D * 2;
+    if (r0 + ROWS <= end) {
+      const T* pa = a + (r0 + w0) * row_a;
+      const T* pb = b + (r0 + w0) * row_b;
+#pragma unroll
+      for (int j = 0; j < UPW; ++j) {
+        const int rows = j / NV * STEP;
+        const unsigned at = dst + (unsigned)((rows + j % NV * RPU) * 2 * D);
+        copy_to_lds16_sb<OWN>(pa + rows * row_a, va[j % NV], at);
+        copy_to_lds16_sb<OWN>(pb + rows * row_b, vb[j % NV], at + TILE);
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < UPW; ++j) {
+        const int rows = j / NV * STEP + j % NV * RPU, r = first + rows;
+        int64_t at = r0 + r;
+        if (at > end - 1) at = end - 1;
+        const int ch = 8 * (lane_chunk ^ swz<D>(r));
+        copy_to_lds16<OWN>(a + at * row_a + ch, dst + (unsigned)(rows * 2 * D));
+        copy_to_lds16<OWN>(b + at * row_b + ch, dst + (unsigned)(rows * 2 * D) + TILE);
+      }
+    }
+  }
+};
 
 // A value of the bias table, times log2 e.
 __device__ __forceinline__ float table_value(const ScoreArgs& s, int bucket, int head) {
@@ -177,15 +239,19 @@ __device__ __forceinline__ float cap_tanh(const ScoreArgs& s, float x) {
   return t;
 }
 
-// Keys visible to a query by position: [0, lim).
-__device__ __forceinline__ int64_t key_limit(const ScoreArgs& s, int b, int64_t n_kv, int64_t pos) {
-  if (!s.causal) return n_kv;
-  int64_t lim = pos + 1;
-  if (s.prefix && s.prefix[b] > lim) lim = s.prefix[b];
+// Keys visible to a query by position: [0, lim).  reach: keys that every query sees
+// (a prefix; all of them without the causal mask).
+__device__ __forceinline__ int64_t key_limit(int64_t n_kv, int64_t reach, int64_t pos) {
+  const int64_t lim = pos + 1 > reach ? pos + 1 : reach;
   return lim < n_kv ? lim : n_kv;
 }
 __device__ __forceinline__ int64_t first_pos(const ScoreArgs& s, int b) {
   const int p = s.q_pos ? s.q_pos[b] : 0;
+  return p > 0 ? p : 0;
+}
+__device__ __forceinline__ int64_t key_reach(const ScoreArgs& s, int b, int64_t n_k) {
+  if (!s.causal) return n_k;
+  const int p = s.prefix ? s.prefix[b] : 0;
   return p > 0 ? p : 0;
 }
 __device__ __forceinline__ int64_t batch_keys(const ScoreArgs& s, int b, int64_t n_k) {
@@ -193,12 +259,6 @@ __device__ __forceinline__ int64_t batch_keys(const ScoreArgs& s, int b, int64_t
   const int64_t l = s.kv_len[b];
   return l < 0 ? 0 : (l > n_k ? n_k : l);
 }
-// A difference of positions as an int that still orders and clamps right.
-__device__ __forceinline__ int rel(int64_t x) {
-  constexpr int64_t kFar = (int64_t)1 << 30;
-  return (int)(x < -kFar ? -kFar : (x > kFar ? kFar : x));
-}
-
 // Smallest and largest id of a wave's 64 lanes.
 __device__ __forceinline__ int2 wave_range(int lo, int hi) {
 #pragma unroll
@@ -229,16 +289,22 @@ __device__ __forceinline__ int4 workgroup_ids(int id, int wave, int lane, int4* 
                    __builtin_amdgcn_readfirstlane(a.z), 0);
 }
 
-// A fragment without the elements whose bits are set, whatever they hold.
-template <typename T>
-__device__ __forceinline__ Frag<T> without(Frag<T> a, uint32_t bits) {
+// Zeroes the rows of two staged tiles whose tokens have no document (the tiles' rows
+// are tokens r0 .., from `end` on the last one before it again), so that whatever they
+// hold meets weights of 0 as a number.  nt threads, for rows [first, first + rows); the caller synchronises.
+template <typename T, int D, int RSA, int RSB, int PA, int PB, int NP>
+__device__ __forceinline__ void zero_absent(T* a, T* b, const int* ids, int64_t r0, int64_t end, int first, int rows, int tid,
+                                            int nt) {
+  for (int i = tid; i < rows * (D / 8); i += nt) {
+    const int r = first + i / (D / 8), x = 8 * (i % (D / 8));
+    if (ids[r0 + r < end ? r0 + r : end - 1] < 0) {
 #pragma unroll
-  for (int e = 0; e < 8; ++e)
-    if (bits >> e & 1) {
-      if constexpr (sizeof(T) == 4) a.p[0][e] = a.p[1][e] = a.p[2][e] = (__bf16)0.0f;
-      else a[e] = (T)0.0f;
+      for (int y = 0; y < NP; ++y) {
+        st16(a + y * PA + r * RSA + x, u32x4{0, 0, 0, 0});
+        st16(b + y * PB + r * RSB + x, u32x4{0, 0, 0, 0});
+      }
     }
-  return a;
+  }
 }
 
 // Tiles of one side that may meet the ids [lo, hi]: 64 tiles at a time, a bit each.
@@ -279,12 +345,8 @@ struct DocTiles {
     }
     return end;
   }
-  // Whether a tile holds the ids [lo, hi] only, all the same.
-  __device__ __forceinline__ bool uniform(int t) const {
-    if (!range) return true;
-    const int2 x = of_tile(t);
-    return lo == hi && x.x == lo && x.y == lo;
-  }
+  // Whether a tile holds other ids than [lo, hi], all the same; and one below 0.
+  __device__ __forceinline__ bool mixed(int2 of) const { return !(lo == hi && of.x == lo && of.y == lo); }
 };
 
 // Arguments of the backward kernels.

@@ -161,6 +161,7 @@ StreamParams stream_params(const mea_problem* p, const ScoreArgs& s, int64_t kv_
   q.n_groups = (int)pl.groups;
   q.n_splits = (int)pl.splits;
   q.scale_log2 = p->scale * kLog2e;
+  q.slack = mea::kRescaleSlack;
   return q;
 }
 
@@ -266,6 +267,7 @@ mea_status mea_scored_attention_fwd(const mea_problem* p, const mea_score* s, co
   a.o = o;
   a.lse = lse;
   a.o_lo = o_lo;
+  if (o_lo) a.slack = 0.0f;
   {
     const mea_strides* t = p->strides;
     const size_t e = elem_size(p->dtype);

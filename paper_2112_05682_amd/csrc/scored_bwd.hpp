@@ -101,7 +101,7 @@ __global__ __launch_bounds__(256, (ScoredKvTile<T, D>::OCC)) void scored_dkdv_ke
   const int64_t k0 = (int64_t)item.tile * C::BKG, kw = k0 + 32 * wave, key = kw + c;
 
   const int64_t n_kv = batch_keys(sa, b, p.n_k), pos0 = first_pos(sa, b);
-  const int64_t reach = sa.causal ? (sa.prefix ? (int64_t)sa.prefix[b] : 0) : p.n_k;  // keys that every query sees
+  const int64_t reach = key_reach(sa, b, p.n_k);
   bool live = key < n_kv;
   int doc = -2;
   int4 ids = make_int4(0, 0, 0, 0);
@@ -116,9 +116,8 @@ __global__ __launch_bounds__(256, (ScoredKvTile<T, D>::OCC)) void scored_dkdv_ke
   // The first query that sees this lane's key, and (uniform) the first one of the
   // workgroup's first key, of its last, and of the wave's first.
   auto first_query = [&](int64_t j) { return j < reach || j <= pos0 ? (int64_t)0 : j - pos0; };
-  const int64_t min_q = live ? first_query(key) : p.n_q;
+  const int min_q = live ? (int)first_query(key) : 0;
   const int64_t q_begin = first_query(k0), q_full = first_query(k0 + C::BKG - 1), qw_begin = first_query(kw);
-  const bool all_live = k0 + C::BKG <= n_kv && ids.z == 0;
 
   const T* __restrict__ kg = static_cast<const T*>(p.k) + (int64_t)b * p.sk.b + (int64_t)kvh * p.sk.h;
   const T* __restrict__ vg = static_cast<const T*>(p.v) + (int64_t)b * p.sv.b + (int64_t)kvh * p.sv.h;
@@ -168,8 +167,8 @@ __global__ __launch_bounds__(256, (ScoredKvTile<T, D>::OCC)) void scored_dkdv_ke
   t = first_tile();
   if (t >= t_end) g = p.heads_per_kv;  // no query sees these keys
 
-  constexpr int CPR = C::CPR, RPU = 64 / CPR, UPW = F32 ? 1 : BQ / RPU / 4;
-  const int urow = lane / CPR, uch = lane % CPR;
+  constexpr int CPR = C::CPR;
+  const TileCopy<std::conditional_t<F32, __bf16, T>, D, BQ, false> copies(wave, lane, p.sq.r, p.sdo.r);
   auto head_of = [&](int g_) { return kvh * p.heads_per_kv + g_; };
   float stage_f = 0.0f;
   auto load_rows = [&](int g_, int t_) __attribute__((always_inline)) {
@@ -183,18 +182,10 @@ __global__ __launch_bounds__(256, (ScoredKvTile<T, D>::OCC)) void scored_dkdv_ke
   };
   // 16-bit: asynchronous copies into swizzled rows; rows past n_q repeat the last.
   auto copy_tile = [&](int g_, int t_, int buf) __attribute__((always_inline)) {
-    const T* qg = static_cast<const T*>(p.q) + (int64_t)b * p.sq.b + (int64_t)head_of(g_) * p.sq.h;
-    const T* og = static_cast<const T*>(p.d_o) + (int64_t)b * p.sdo.b + (int64_t)head_of(g_) * p.sdo.h;
-    const unsigned base = __builtin_amdgcn_readfirstlane(lds_addr(smem + buf * C::STAGE_BYTES));
-#pragma unroll
-    for (int j = 0; j < UPW; ++j) {
-      const int u = wave + 4 * j, r = RPU * u + urow;
-      int64_t qi = (int64_t)t_ * BQ + r;
-      if (qi > p.n_q - 1) qi = p.n_q - 1;
-      const int ch = 8 * (uch ^ swz<D>(r));
-      copy_to_lds16(qg + qi * p.sq.r + ch, base + 1024u * (unsigned)u);
-      copy_to_lds16(og + qi * p.sdo.r + ch, base + (unsigned)C::TILE_BYTES + 1024u * (unsigned)u);
-    }
+    if constexpr (!F32)
+      copies(static_cast<const T*>(p.q) + (int64_t)b * p.sq.b + (int64_t)head_of(g_) * p.sq.h, p.sq.r,
+             static_cast<const T*>(p.d_o) + (int64_t)b * p.sdo.b + (int64_t)head_of(g_) * p.sdo.h, p.sdo.r,
+             (int64_t)t_ * BQ, p.n_q, __builtin_amdgcn_readfirstlane(lds_addr(smem + buf * C::STAGE_BYTES)), wave);
   };
   Chunk8<T> stage[F32 ? C::CPT : 1];
   auto load_stage = [&](int g_, int t_) __attribute__((always_inline)) {
@@ -231,42 +222,50 @@ __global__ __launch_bounds__(256, (ScoredKvTile<T, D>::OCC)) void scored_dkdv_ke
   const float cl2 = p.scale_log2;
   float slope2 = 0.0f;
 
-  auto compute = [&](auto mask_tag, int t_, int buf, bool one_doc) {
-    constexpr bool MASK = decltype(mask_tag)::value;
+  // One tile of queries: masked, some query sees some key of the workgroup not; by_doc,
+  // documents differ (uniform branches of one copy of the code, as in the forward).
+  auto compute = [&](int t_, int buf, bool masked, bool by_doc) __attribute__((always_inline)) {
     const int64_t q0t = (int64_t)t_ * BQ;
     if (q0t + BQ <= qw_begin || kw >= n_kv) return;  // none of the wave's keys is seen
     const unsigned char* st = smem + buf * C::STAGE_BYTES;
-    const float* lse_s = reinterpret_cast<const float*>(st + 2 * C::TILE_BYTES);
-    const float* nd_s = lse_s + BQ;
-#pragma unroll
+#pragma unroll 1
     for (int qs = 0; qs < QS; ++qs) {
       const int64_t q0 = q0t + 32 * qs;
       const unsigned char* qt = st + qs * 32 * (2 * D);
       const unsigned char* ot = qt + C::TILE_BYTES;
       const LE* qt32 = reinterpret_cast<const LE*>(st) + qs * 32 * C::RS;
       const LE* ot32 = reinterpret_cast<const LE*>(st + C::TILE_BYTES) + qs * 32 * C::RS;
+      const float* lse_s = reinterpret_cast<const float*>(st + 2 * C::TILE_BYTES) + 32 * qs + 8 * h;
       f32x16 s, dp;
-      float l2[16];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const int row = 32 * qs + 16 * (j >> 1) + 8 * h + 4 * (j & 1);
-        const f32x4 a = *reinterpret_cast<const f32x4*>(lse_s + row);
-        const f32x4 d = *reinterpret_cast<const f32x4*>(nd_s + row);
+        const f32x4 d = *reinterpret_cast<const f32x4*>(lse_s + BQ + 16 * (j >> 1) + 4 * (j & 1));
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           s[4 * j + e] = 0.0f;
-          l2[4 * j + e] = a[e];
           dp[4 * j + e] = d[e];
         }
       }
+      if constexpr (F32) {
 #pragma unroll
-      for (int kc = 0; kc < KC; ++kc) {
-        if constexpr (F32) {
+        for (int kc = 0; kc < KC; ++kc) {
           s = mma(lds_frag_planes<T>(qt32 + qrow * C::RS + 16 * kc + 8 * h, C::TILE), kfrag(kc), s);
           dp = mma(lds_frag_planes<T>(ot32 + qrow * C::RS + 16 * kc + 8 * h, C::TILE), vf[kc], dp);
-        } else {
-          s = mma(row_frag<T, D>(qt, qrow, 2 * kc + h), kfrag(kc), s);
-          dp = mma(row_frag<T, D>(ot, qrow, 2 * kc + h), vf[kc], dp);
+        }
+      } else {
+        // Fragments are read one chunk before their MFMAs, and not earlier (registers).
+        Frag<T> fa[2], fg[2];
+        fa[0] = row_frag<T, D>(qt, qrow, h);
+        fg[0] = row_frag<T, D>(ot, qrow, h);
+#pragma unroll
+        for (int kc = 0; kc < KC; ++kc) {
+          if (kc + 1 < KC) {
+            fa[(kc + 1) & 1] = row_frag<T, D>(qt, qrow, 2 * (kc + 1) + h);
+            fg[(kc + 1) & 1] = row_frag<T, D>(ot, qrow, 2 * (kc + 1) + h);
+          }
+          s = mma(fa[kc & 1], kfrag(kc), s);
+          dp = mma(fg[kc & 1], vf[kc], dp);
+          __builtin_amdgcn_sched_barrier(0);
         }
       }
       float grad[CAP ? 16 : 1];  // 1 - tanh^2
@@ -283,11 +282,11 @@ __global__ __launch_bounds__(256, (ScoredKvTile<T, D>::OCC)) void scored_dkdv_ke
         }
       }
       if constexpr (BIAS) {
-        const int off = rel(key - (pos0 + q0));  // distance to the tile's first query
+        const int off = (int)key - (int)(pos0 + q0) - 8 * h;  // distance to the tile's first query, less 8 h
         if (sa.slopes) {
           const float d0 = (float)off;
 #pragma unroll
-          for (int r = 0; r < 16; ++r) s[r] = fmaf(-fabsf(d0 - (float)permuted_row(r, h)), slope2, s[r]);
+          for (int r = 0; r < 16; ++r) s[r] = fmaf(-fabsf(d0 - (float)permuted_row(r, 0)), slope2, s[r]);
         }
         if (sa.table) {
           const int hi = sa.two_sided ? sa.span : 0, last = bias_places(sa) - 1;
@@ -297,77 +296,63 @@ __global__ __launch_bounds__(256, (ScoredKvTile<T, D>::OCC)) void scored_dkdv_ke
 #pragma unroll
             for (int r = 0; r < 16; ++r) s[r] += x;
           } else {
+            asm volatile("");
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-              int d = off - permuted_row(r, h);
+              int d = off - permuted_row(r, 0);
               d = d < -sa.span ? -sa.span : (d > hi ? hi : d);
               s[r] += reinterpret_cast<const float*>(lds_bias)[d + sa.span];
             }
           }
         }
       }
-      // P and dS; absent: rows without a document (bit 8 m + e: row 16 m + 8 h + e).
-      uint32_t absent = 0;
-      float pr[16];
+      if (masked) {
+        asm volatile("");
+        const int m = min_q - (int)q0 - 8 * h;
 #pragma unroll
-      for (int r = 0; r < 16; ++r) pr[r] = fast_exp2(LOG2 ? s[r] - l2[r] : fmaf(s[r], cl2, -l2[r]));
-      if constexpr (MASK) {
-        const int m = rel(min_q - q0);
-        int mine = 0;
-        const bool by_doc = sa.q_doc && !one_doc;
-        if (by_doc) mine = q0 + c < p.n_q ? sa.q_doc[(int64_t)b * p.n_q + q0 + c] : -1;
+        for (int r = 0; r < 16; ++r)
+          if (permuted_row(r, 0) < m) s[r] = -INFINITY;
+      }
+      if (by_doc) {
+        asm volatile("");
+        const int mine = q0 + c < p.n_q ? sa.q_doc[(int64_t)b * p.n_q + q0 + c] : -1;
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          bool off_ = permuted_row(r, h) < m;
-          if (by_doc) {
-            const int id = __shfl(mine, permuted_row(r, h));
-            off_ = off_ || id != doc;
-            if (id < 0) absent |= 1u << r;
-          }
-          pr[r] = off_ ? 0.0f : pr[r];
-          dp[r] = off_ ? 0.0f : pr[r] * dp[r];
-          if constexpr (CAP) grad[r] = off_ ? 0.0f : grad[r];  // a hidden score may be NaN
+          const int id = __shfl(mine, permuted_row(r, h));
+          if (id != doc) s[r] = -INFINITY;
         }
-      } else {
-#pragma unroll
-        for (int r = 0; r < 16; ++r) dp[r] *= pr[r];
       }
-      if constexpr (CAP)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) dp[r] *= grad[r];
-      const bool drop = MASK && __builtin_amdgcn_ballot_w64(absent != 0);
-      // dV^T += dO^T P and dK^T += Q^T dX.
+      // P, dS and dX, rounded to the operands of the products with dO and Q.
       Frag<T> pf[2], sf[2];
 #pragma unroll
       for (int m = 0; m < 2; ++m) {
         float x[8], y[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          x[e] = pr[8 * m + e];
-          y[e] = dp[8 * m + e];
+        for (int j = 0; j < 2; ++j) {
+          const f32x4 l2 = *reinterpret_cast<const f32x4*>(lse_s + 16 * m + 4 * j);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int r = 8 * m + 4 * j + e;
+            x[4 * j + e] = fast_exp2(LOG2 ? s[r] - l2[e] : fmaf(s[r], cl2, -l2[e]));
+            y[4 * j + e] = x[4 * j + e] * dp[r];
+            if constexpr (CAP) y[4 * j + e] *= grad[r];
+          }
         }
         pf[m] = to_frag<T>(x);
         sf[m] = to_frag<T>(y);
       }
+      // dV^T += dO^T P and dK^T += Q^T dX.
 #pragma unroll
-      for (int dt = 0; dt < NDT; ++dt)
+      for (int m = 0; m < 2; ++m)
 #pragma unroll
-        for (int m = 0; m < 2; ++m) {
-          Frag<T> a, e;
+        for (int dt = 0; dt < NDT; ++dt) {
           if constexpr (F32) {
-            a = lds_col_frag_planes<T>(ot32, C::TILE, C::RS, 16 * m, 32 * dt, lane);
-            e = lds_col_frag_planes<T>(qt32, C::TILE, C::RS, 16 * m, 32 * dt, lane);
+            dv[dt] = mma(lds_col_frag_planes<T>(ot32, C::TILE, C::RS, 16 * m, 32 * dt, lane), pf[m], dv[dt]);
+            dk[dt] = mma(lds_col_frag_planes<T>(qt32, C::TILE, C::RS, 16 * m, 32 * dt, lane), sf[m], dk[dt]);
           } else {
-            a = col_frag<T, D>(ot, 16 * m, 32 * dt, lane);
-            e = col_frag<T, D>(qt, 16 * m, 32 * dt, lane);
+            dv[dt] = mma(col_frag<T, D>(ot, 16 * m, 32 * dt, lane), pf[m], dv[dt]);
+            dk[dt] = mma(col_frag<T, D>(qt, 16 * m, 32 * dt, lane), sf[m], dk[dt]);
           }
-          if constexpr (MASK)
-            if (drop) {
-              a = without<T>(a, absent >> (8 * m));
-              e = without<T>(e, absent >> (8 * m));
-            }
-          dv[dt] = mma(a, pf[m], dv[dt]);
-          dk[dt] = mma(e, sf[m], dk[dt]);
         }
     }
   };
@@ -385,8 +370,13 @@ __global__ __launch_bounds__(256, (ScoredKvTile<T, D>::OCC)) void scored_dkdv_ke
   }
   if constexpr (F32) __syncthreads();
   while (g < p.heads_per_kv) {
-    const bool one_doc = ids.z == 0 && docs.uniform(t);
-    const bool plain = all_live && one_doc && (int64_t)t * BQ >= q_full;
+    const bool masked = (int64_t)t * BQ < q_full;
+    bool by_doc = false, absent = false;
+    if (sa.q_doc) {
+      const int2 of = docs.of_tile(t);
+      by_doc = ids.z || docs.mixed(of);
+      absent = of.x < 0;
+    }
     int gn = g, tn = t;
     advance(gn, tn);
     const bool more = gn < p.heads_per_kv;
@@ -409,8 +399,14 @@ __global__ __launch_bounds__(256, (ScoredKvTile<T, D>::OCC)) void scored_dkdv_ke
       if constexpr (F32) load_stage(gn, tn);
       else copy_tile(gn, tn, buf ^ 1);
     }
-    if (plain) compute(std::false_type{}, t, buf, true);
-    else compute(std::true_type{}, t, buf, one_doc);
+    if (absent) {
+      LE* st = reinterpret_cast<LE*>(smem + buf * C::STAGE_BYTES);
+      constexpr int RS = F32 ? C::RS : D, PL = F32 ? C::TILE : 0;
+      zero_absent<LE, D, RS, RS, PL, PL, F32 ? C::NP : 1>(st, st + C::TILE_BYTES / 2, sa.q_doc + (int64_t)b * p.n_q, (int64_t)t * BQ,
+                                                         p.n_q, 0, BQ, tid, C::NT);
+      __syncthreads();
+    }
+    compute(t, buf, masked, by_doc);
     const int nb = NBUF == 2 ? buf ^ 1 : 0;
     if constexpr (F32) {
       if (NBUF == 1) __syncthreads();
@@ -497,10 +493,12 @@ __global__ __launch_bounds__(256, (ScoredDqTile<T, D>::OCC)) void scored_dq_kern
   const int64_t row = ((int64_t)b * sa.heads + head) * p.n_q_pad + qi;
   const bool in_rows = qi < p.n_q;
   const float l2 = in_rows ? p.lse2[row] : INFINITY, neg_d = in_rows ? p.neg_d[row] : 0.0f;
-  int64_t lim = in_rows && l2 != INFINITY ? key_limit(sa, b, n_kv, pos0 + qi) : 0;
-  const int64_t lim_hi = key_limit(sa, b, n_kv, pos0 + q_last), lim_lo = key_limit(sa, b, n_kv, pos0 + q0);
+  const int64_t reach = key_reach(sa, b, p.n_k);
+  const int pos = (int)(pos0 + qi);
+  int lim = in_rows && l2 != INFINITY ? (int)key_limit(n_kv, reach, pos0 + qi) : 0;
+  const int64_t lim_hi = key_limit(n_kv, reach, pos0 + q_last), lim_lo = key_limit(n_kv, reach, pos0 + q0);
   const int64_t w_last = qw + 31 < p.n_q ? qw + 31 : p.n_q - 1;
-  const int64_t w_lim = qw < p.n_q ? key_limit(sa, b, n_kv, pos0 + w_last) : 0;
+  const int64_t w_lim = qw < p.n_q ? key_limit(n_kv, reach, pos0 + w_last) : 0;
 
   int doc = -2;
   int4 ids = make_int4(0, 0, 0, 0);
@@ -551,19 +549,12 @@ __global__ __launch_bounds__(256, (ScoredDqTile<T, D>::OCC)) void scored_dq_kern
   wait_global_loads();
   __syncthreads();  // the bias is there
 
-  constexpr int CPR = C::CPR, RPU = 64 / CPR, UPW = F32 ? 1 : BK / RPU / 4;
-  const int urow = lane / CPR, uch = lane % CPR;
+  constexpr int CPR = C::CPR;
+  const TileCopy<std::conditional_t<F32, __bf16, T>, D, BK, false> copies(wave, lane, p.sk.r, p.sv.r);
   auto copy_tile = [&](int t, int buf) __attribute__((always_inline)) {
-    const unsigned base = __builtin_amdgcn_readfirstlane(lds_addr(smem + buf * C::STAGE_BYTES));
-#pragma unroll
-    for (int j = 0; j < UPW; ++j) {
-      const int u = wave + 4 * j, r = RPU * u + urow;
-      int64_t key = (int64_t)t * BK + r;
-      if (key > lim_hi - 1) key = lim_hi - 1;
-      const int ch = 8 * (uch ^ swz<D>(r));
-      copy_to_lds16(kg + key * p.sk.r + ch, base + 1024u * (unsigned)u);
-      copy_to_lds16(vg + key * p.sv.r + ch, base + (unsigned)C::TILE_BYTES + 1024u * (unsigned)u);
-    }
+    if constexpr (!F32)
+      copies(kg, p.sk.r, vg, p.sv.r, (int64_t)t * BK, lim_hi,
+             __builtin_amdgcn_readfirstlane(lds_addr(smem + buf * C::STAGE_BYTES)), wave);
   };
   Chunk8<T> stage[F32 ? C::CPT : 1];
   auto load_stage = [&](int t) __attribute__((always_inline)) {
@@ -598,10 +589,9 @@ __global__ __launch_bounds__(256, (ScoredDqTile<T, D>::OCC)) void scored_dq_kern
   const float cl2 = p.scale_log2;
   const int64_t p_lo = pos0 + qw, p_hi = pos0 + w_last;  // the wave's positions
 
-  auto tile = [&](auto mask_tag, int t, int buf, bool one_doc) {
-    constexpr bool MASK = decltype(mask_tag)::value;
+  auto tile = [&](int t, int buf, bool masked, bool by_doc) __attribute__((always_inline)) {
     const unsigned char* st = smem + buf * C::STAGE_BYTES;
-#pragma unroll
+#pragma unroll 1
     for (int kt = 0; kt < NKT; ++kt) {
       const int64_t k0 = (int64_t)t * BK + 32 * kt;
       if (k0 >= w_lim) return;
@@ -615,14 +605,25 @@ __global__ __launch_bounds__(256, (ScoredDqTile<T, D>::OCC)) void scored_dq_kern
         s[r] = 0.0f;
         dp[r] = neg_d;
       }
+      if constexpr (F32) {
 #pragma unroll
-      for (int kc = 0; kc < KC; ++kc) {
-        if constexpr (F32) {
+        for (int kc = 0; kc < KC; ++kc) {
           s = mma(lds_frag_planes<T>(kt32 + krow * C::RS + 16 * kc + 8 * h, C::TILE), qf[kc], s);
           dp = mma(lds_frag_planes<T>(vt32 + krow * C::RS + 16 * kc + 8 * h, C::TILE), gf[kc], dp);
-        } else {
-          s = mma(row_frag<T, D>(kt16, krow, 2 * kc + h), qf[kc], s);
-          dp = mma(row_frag<T, D>(vt16, krow, 2 * kc + h), gf[kc], dp);
+        }
+      } else {
+        Frag<T> fa[2], fg[2];
+        fa[0] = row_frag<T, D>(kt16, krow, h);
+        fg[0] = row_frag<T, D>(vt16, krow, h);
+#pragma unroll
+        for (int kc = 0; kc < KC; ++kc) {
+          if (kc + 1 < KC) {
+            fa[(kc + 1) & 1] = row_frag<T, D>(kt16, krow, 2 * (kc + 1) + h);
+            fg[(kc + 1) & 1] = row_frag<T, D>(vt16, krow, 2 * (kc + 1) + h);
+          }
+          s = mma(fa[kc & 1], qf[kc], s);
+          dp = mma(fg[kc & 1], gf[kc], dp);
+          __builtin_amdgcn_sched_barrier(0);
         }
       }
       float grad[CAP ? 16 : 1];
@@ -638,14 +639,14 @@ __global__ __launch_bounds__(256, (ScoredDqTile<T, D>::OCC)) void scored_dq_kern
           }
         }
       }
-      const int off = BIAS ? rel(k0 - (pos0 + qi)) : 0;
+      const int off = BIAS ? (int)k0 - pos + 8 * h : 0;
       const int hi = sa.two_sided ? sa.span : 0;
       const bool far = BIAS && (k0 + 31 <= p_lo - sa.span || k0 >= p_hi + hi);
       if constexpr (BIAS) {
         if (sa.slopes) {
           const float d0 = (float)off;
 #pragma unroll
-          for (int r = 0; r < 16; ++r) s[r] = fmaf(-fabsf(d0 + (float)permuted_row(r, h)), slope2, s[r]);
+          for (int r = 0; r < 16; ++r) s[r] = fmaf(-fabsf(d0 + (float)permuted_row(r, 0)), slope2, s[r]);
         }
         if (sa.table) {
           if (far) {
@@ -653,39 +654,34 @@ __global__ __launch_bounds__(256, (ScoredDqTile<T, D>::OCC)) void scored_dq_kern
 #pragma unroll
             for (int r = 0; r < 16; ++r) s[r] += x;
           } else {
+            asm volatile("");
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-              int d = off + permuted_row(r, h);
+              int d = off + permuted_row(r, 0);
               d = d < -sa.span ? -sa.span : (d > hi ? hi : d);
               s[r] += reinterpret_cast<const float*>(lds_bias)[d + sa.span];
             }
           }
         }
       }
-      uint32_t absent = 0;
-      float pr[16];
+      if (masked) {
+        asm volatile("");
+        const int m = lim - (int)k0 - 8 * h;
 #pragma unroll
-      for (int r = 0; r < 16; ++r) pr[r] = fast_exp2(LOG2 ? s[r] - l2 : fmaf(s[r], cl2, -l2));
-      if constexpr (MASK) {
-        const int m = rel(lim - k0);
-        int mine = 0;
-        const bool by_doc = sa.q_doc && !one_doc;
-        if (by_doc) mine = k0 + c < p.n_k ? sa.k_doc[(int64_t)b * p.n_k + k0 + c] : -1;
+        for (int r = 0; r < 16; ++r)
+          if (permuted_row(r, 0) >= m) s[r] = -INFINITY;
+      }
+      if (by_doc) {
+        asm volatile("");
+        const int mine = k0 + c < p.n_k ? sa.k_doc[(int64_t)b * p.n_k + k0 + c] : -1;
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          bool off_ = permuted_row(r, h) >= m;
-          if (by_doc) {
-            const int id = __shfl(mine, permuted_row(r, h));
-            off_ = off_ || id != doc;
-            if (id < 0) absent |= 1u << r;
-          }
-          dp[r] = off_ ? 0.0f : pr[r] * dp[r];
-          if constexpr (CAP) grad[r] = off_ ? 0.0f : grad[r];  // a hidden score may be NaN
+          const int id = __shfl(mine, permuted_row(r, h));
+          if (id != doc) s[r] = -INFINITY;
         }
-      } else {
-#pragma unroll
-        for (int r = 0; r < 16; ++r) dp[r] *= pr[r];
       }
+#pragma unroll
+      for (int r = 0; r < 16; ++r) dp[r] *= fast_exp2(LOG2 ? s[r] - l2 : fmaf(s[r], cl2, -l2));  // dS
       if constexpr (BIAS) {
         if (sums) {
           if (far) {
@@ -696,9 +692,10 @@ __global__ __launch_bounds__(256, (ScoredDqTile<T, D>::OCC)) void scored_dq_kern
             if (k0 >= p_hi + hi) far_hi += x;
             else far_lo += x;
           } else {
+            asm volatile("");
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-              const int d = off + permuted_row(r, h);
+              const int d = off + permuted_row(r, 0);
               if (d <= -sa.span) far_lo += dp[r];
               else if (d >= hi) far_hi += dp[r];
               else lds_add(my_bins + d + sa.span, dp[r]);
@@ -709,7 +706,6 @@ __global__ __launch_bounds__(256, (ScoredDqTile<T, D>::OCC)) void scored_dq_kern
       if constexpr (CAP)
 #pragma unroll
         for (int r = 0; r < 16; ++r) dp[r] *= grad[r];
-      const bool drop = MASK && __builtin_amdgcn_ballot_w64(absent != 0);
       Frag<T> sf[2];
 #pragma unroll
       for (int m = 0; m < 2; ++m) {
@@ -719,15 +715,11 @@ __global__ __launch_bounds__(256, (ScoredDqTile<T, D>::OCC)) void scored_dq_kern
         sf[m] = to_frag<T>(x);
       }
 #pragma unroll
-      for (int dt = 0; dt < NDT; ++dt)
+      for (int m = 0; m < 2; ++m)
 #pragma unroll
-        for (int m = 0; m < 2; ++m) {
-          Frag<T> a;
-          if constexpr (F32) a = lds_col_frag_planes<T>(kt32, C::TILE, C::RS, 16 * m, 32 * dt, lane);
-          else a = col_frag<T, D>(kt16, 16 * m, 32 * dt, lane);
-          if constexpr (MASK)
-            if (drop) a = without<T>(a, absent >> (8 * m));
-          acc[dt] = mma(a, sf[m], acc[dt]);
+        for (int dt = 0; dt < NDT; ++dt) {
+          if constexpr (F32) acc[dt] = mma(lds_col_frag_planes<T>(kt32, C::TILE, C::RS, 16 * m, 32 * dt, lane), sf[m], acc[dt]);
+          else acc[dt] = mma(col_frag<T, D>(kt16, 16 * m, 32 * dt, lane), sf[m], acc[dt]);
         }
     }
   };
@@ -745,8 +737,13 @@ __global__ __launch_bounds__(256, (ScoredDqTile<T, D>::OCC)) void scored_dq_kern
   if constexpr (F32) __syncthreads();
   while (t < t_end) {
     const int tn = docs.next(t + 1, t_end);
-    const bool one_doc = ids.z == 0 && docs.uniform(t);
-    const bool plain = (int64_t)(t + 1) * BK <= lim_lo && one_doc;
+    const bool masked = (int64_t)(t + 1) * BK > lim_lo;
+    bool by_doc = false, absent = false;
+    if (sa.q_doc) {
+      const int2 of = docs.of_tile(t);
+      by_doc = ids.z || docs.mixed(of);
+      absent = of.x < 0;
+    }
     if constexpr (F32) {
       if (tn < t_end) load_stage(tn);
     } else {
@@ -754,8 +751,14 @@ __global__ __launch_bounds__(256, (ScoredDqTile<T, D>::OCC)) void scored_dq_kern
       __syncthreads();
       if (tn < t_end) copy_tile(tn, buf ^ 1);
     }
-    if (plain) tile(std::false_type{}, t, buf, true);
-    else tile(std::true_type{}, t, buf, one_doc);
+    if (absent) {
+      LE* st = reinterpret_cast<LE*>(smem + buf * C::STAGE_BYTES);
+      constexpr int RS = F32 ? C::RS : D, PL = F32 ? C::TILE : 0;
+      zero_absent<LE, D, RS, RS, PL, PL, F32 ? C::NP : 1>(st, st + C::TILE_BYTES / 2, sa.k_doc + (int64_t)b * p.n_k, (int64_t)t * BK,
+                                                         lim_hi, 0, BK, tid, C::NT);
+      __syncthreads();
+    }
+    tile(t, buf, masked, by_doc);
     const int nb = NBUF == 2 ? buf ^ 1 : 0;
     if constexpr (F32) {
       if (NBUF == 1) __syncthreads();

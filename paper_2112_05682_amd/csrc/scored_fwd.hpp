@@ -79,18 +79,20 @@ __global__ __launch_bounds__(256, (StreamTile<T, D, RW>::OCC)) void scored_strea
   const int head = head0 + g;
 
   const int64_t n_kv = batch_keys(sa, b0, p.n_k);
-  const int64_t pos0 = first_pos(sa, b0);
-  int64_t lim = in_rows ? key_limit(sa, b0, n_kv, pos0 + qi) : 0;
+  const int64_t pos0 = first_pos(sa, b0), reach = key_reach(sa, b0, p.n_k);
+  // Keys and positions are below 2^31, so that per-lane ones are 32 bits.
+  const int pos = (int)(pos0 + qi);
+  int lim = in_rows ? (int)key_limit(n_kv, reach, pos0 + qi) : 0;
   // Limits grow with the query, so the tile's first and last rows bound them (a
   // group of several batches has no positional mask).
-  const int64_t lim_hi = key_limit(sa, b0, n_kv, pos0 + (row_last / p.fold) % p.n_q);
-  const int64_t lim_lo = key_limit(sa, b0, n_kv, pos0 + (row0 / p.fold) % p.n_q);
+  const int64_t lim_hi = key_limit(n_kv, reach, pos0 + (row_last / p.fold) % p.n_q);
+  const int64_t lim_lo = key_limit(n_kv, reach, pos0 + (row0 / p.fold) % p.n_q);
   const int64_t w_row0 = row0 + 32 * wave_q;
   const int64_t w_last = w_row0 + 31 < p.group_rows ? w_row0 + 31 : p.group_rows - 1;
   // The wave's first and last query (uniform), and its limit.
   const bool wave_rows = w_row0 < p.group_rows;
   const int64_t wq_lo = pos0 + w_row0 / p.fold % p.n_q, wq_hi = pos0 + (wave_rows ? w_last / p.fold % p.n_q : 0);
-  const int64_t w_lim = wave_rows ? key_limit(sa, b0, n_kv, wq_hi) : 0;
+  const int64_t w_lim = wave_rows ? key_limit(n_kv, reach, wq_hi) : 0;
 
   int doc = -2;
   int4 ids = make_int4(0, 0, 0, 0);
@@ -139,23 +141,13 @@ __global__ __launch_bounds__(256, (StreamTile<T, D, RW>::OCC)) void scored_strea
 
   // ---- staging.  16-bit: copies of 1 KiB, rows past the last visible key repeat
   // it (finite, and masked); with RW = 1 each wave copies its own keys.
-  constexpr int CPR = C::CPR, RPU = 64 / CPR;
+  constexpr int CPR = C::CPR;
   constexpr bool OWN = RW == 1;
-  constexpr int UNITS_K = BK / RPU, UPW = UNITS_K / 4;  // copies of K (and of V) per tile and wave
-  const int urow = lane / CPR, uch = lane % CPR;
+  const TileCopy<std::conditional_t<F32, __bf16, T>, D, BK, OWN> copies(wave, lane, p.sk.r, p.sv.r);
   auto copy_tile = [&](int t, int buf) __attribute__((always_inline)) {
-    const int64_t k0 = (int64_t)t * BK;
-    const unsigned base = __builtin_amdgcn_readfirstlane(lds_addr(smem + buf * C::STAGE_BYTES));
-#pragma unroll
-    for (int j = 0; j < UPW; ++j) {
-      const int u = OWN ? wave * UPW + j : wave + 4 * j;
-      const int r = RPU * u + urow;
-      int64_t key = k0 + r;
-      if (key > lim_hi - 1) key = lim_hi - 1;
-      const int ch = 8 * (uch ^ swz<D>(r));
-      copy_to_lds16<OWN>(kg + key * p.sk.r + ch, base + 1024u * (unsigned)u);
-      copy_to_lds16<OWN>(vg + key * p.sv.r + ch, base + (unsigned)(BK * D * 2) + 1024u * (unsigned)u);
-    }
+    if constexpr (!F32)
+      copies(kg, p.sk.r, vg, p.sv.r, (int64_t)t * BK, lim_hi,
+             __builtin_amdgcn_readfirstlane(lds_addr(smem + buf * C::STAGE_BYTES)), wave);
   };
   Chunk8<T> stage[F32 ? C::CPT : 1];
   auto load_stage = [&](int t) __attribute__((always_inline)) {
@@ -190,8 +182,11 @@ __global__ __launch_bounds__(256, (StreamTile<T, D, RW>::OCC)) void scored_strea
   const int krow = perm32(c);
   const float cl2 = p.scale_log2;
 
-  auto tile = [&](auto mask_tag, int t, int buf, bool one_doc) {
-    constexpr bool MASK = decltype(mask_tag)::value;
+  // One tile: masked, some key is beyond some row's limit; by_doc, documents differ.
+  // The masks are uniform branches (an empty volatile statement each, so that they do
+  // not become selects in every tile) of one copy of the code: with a copy each for
+  // plain and masked tiles the d = 64 kernels spilled 84-173 registers in the loop.
+  auto tile = [&](int t, int buf, bool masked, bool by_doc) __attribute__((always_inline)) {
     const int64_t k0 = (int64_t)t * BK + BKW * wave_k;
     if (k0 >= w_lim) return;  // all keys beyond this wave's rows
     const unsigned char* st = smem + buf * C::STAGE_BYTES;
@@ -230,14 +225,13 @@ __global__ __launch_bounds__(256, (StreamTile<T, D, RW>::OCC)) void scored_strea
         for (int r = 0; r < 16; ++r) s[kt][r] = CAP ? sa.cap2 * cap_tanh<T>(sa, s[kt][r]) : s[kt][r] * cl2;
     }
     if constexpr (BIAS) {
-      const int off = rel(k0 - (pos0 + qi));  // first key's distance
+      const int off = (int)k0 - pos;  // first key's distance
       if (sa.slopes) {
-        const float d0 = (float)off;
+        const float d0 = (float)(off + 8 * h);
 #pragma unroll
         for (int kt = 0; kt < NKT; ++kt)
 #pragma unroll
-          for (int r = 0; r < 16; ++r)
-            s[kt][r] = fmaf(-fabsf(d0 + (float)(32 * kt + permuted_row(r, h))), slope2, s[kt][r]);
+          for (int r = 0; r < 16; ++r) s[kt][r] = fmaf(-fabsf(d0 + (float)(32 * kt + permuted_row(r, 0))), slope2, s[kt][r]);
       }
       if (sa.table) {
         const int hi = sa.two_sided ? sa.span : 0, last = bias_places(sa) - 1;
@@ -249,6 +243,7 @@ __global__ __launch_bounds__(256, (StreamTile<T, D, RW>::OCC)) void scored_strea
 #pragma unroll
             for (int r = 0; r < 16; ++r) s[kt][r] += v;
           } else {
+            asm volatile("");
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
               int d = off + 32 * kt + permuted_row(r, h);
@@ -260,27 +255,26 @@ __global__ __launch_bounds__(256, (StreamTile<T, D, RW>::OCC)) void scored_strea
       }
     }
 
-    // Masks.  absent: bit e of byte pc, key 16 pc + 8 h + e has no document.
-    uint32_t absent = 0;
-    static_assert(NPC <= 4, "a byte for each 16 keys");
-    if constexpr (MASK) {
-      const int l = rel(lim - k0);
+    // Masks.
+    if (masked) {
+      asm volatile("");
+      const int l = lim - (int)k0 - 8 * h;
 #pragma unroll
       for (int kt = 0; kt < NKT; ++kt)
 #pragma unroll
         for (int r = 0; r < 16; ++r)
-          if (32 * kt + permuted_row(r, h) >= l) s[kt][r] = -INFINITY;
-      if (sa.q_doc && !one_doc) {
+          if (32 * kt + permuted_row(r, 0) >= l) s[kt][r] = -INFINITY;
+    }
+    if (by_doc) {
+      asm volatile("");
 #pragma unroll
-        for (int kt = 0; kt < NKT; ++kt) {
-          const int64_t key = k0 + 32 * kt + c;
-          const int mine = key < p.n_k ? sa.k_doc[(int64_t)b0 * p.n_k + key] : -1;
+      for (int kt = 0; kt < NKT; ++kt) {
+        const int64_t key = k0 + 32 * kt + c;
+        const int mine = key < p.n_k ? sa.k_doc[(int64_t)b0 * p.n_k + key] : -1;
 #pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const int id = __shfl(mine, permuted_row(r, h));
-            if (id != doc) s[kt][r] = -INFINITY;
-            if (id < 0) absent |= 1u << (8 * (2 * kt + r / 8) + r % 8);
-          }
+        for (int r = 0; r < 16; ++r) {
+          const int id = __shfl(mine, permuted_row(r, h));
+          if (id != doc) s[kt][r] = -INFINITY;
         }
       }
     }
@@ -293,7 +287,7 @@ __global__ __launch_bounds__(256, (StreamTile<T, D, RW>::OCC)) void scored_strea
       for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[kt][r]);
     const float mul = LOG2 ? 1.0f : cl2;
     const float mx_c = xhalf_max(mx) * mul;
-    const bool raise = mx_c > m_ref + kRescaleSlack;
+    const bool raise = mx_c > m_ref + p.slack;
     if (__builtin_amdgcn_ballot_w64(raise)) {
       const float m_new = raise ? mx_c : m_ref;
       const float alpha = raise ? fast_exp2(m_ref - m_new) : 1.0f;
@@ -304,7 +298,8 @@ __global__ __launch_bounds__(256, (StreamTile<T, D, RW>::OCC)) void scored_strea
         for (int r = 0; r < 16; ++r) acc[dt][r] *= alpha;
       m_ref = m_new;
     }
-    const float neg = (MASK && m_ref == -INFINITY) ? 0.0f : -m_ref;
+    // A row with no visible key so far: its (all -inf) exponents get weight 0.
+    const float neg = m_ref == -INFINITY ? 0.0f : -m_ref;
     Frag<T> pf[NPC];
 #pragma unroll
     for (int pc = 0; pc < NPC; ++pc) {
@@ -317,20 +312,14 @@ __global__ __launch_bounds__(256, (StreamTile<T, D, RW>::OCC)) void scored_strea
       pf[pc] = to_frag<T>(e8);
       l_run = tree_sum<8>(e8, l_run);
     }
-    // O^T += V^T P^T; keys without a document are taken out of V, whatever they hold.
-    const bool drop = MASK && __builtin_amdgcn_ballot_w64(absent != 0);
+    // O^T += V^T P^T.
 #pragma unroll
     for (int dt = 0; dt < NDT; ++dt) {
       f32x16 sum = {};
 #pragma unroll
       for (int pc = 0; pc < NPC; ++pc) {
-        Frag<T> a;
-        if constexpr (F32) a = lds_col_frag_planes<T>(vs, C::TILEV, C::RSV, 16 * pc, 32 * dt, lane);
-        else a = col_frag<T, D>(vt16, 16 * pc, 32 * dt, lane);
-        if constexpr (MASK)
-          if (drop) a = without<T>(a, absent >> (8 * pc));
-        if constexpr (F32) sum = mma(a, pf[pc], sum);
-        else acc[dt] = mma(a, pf[pc], acc[dt]);
+        if constexpr (F32) sum = mma(lds_col_frag_planes<T>(vs, C::TILEV, C::RSV, 16 * pc, 32 * dt, lane), pf[pc], sum);
+        else acc[dt] = mma(col_frag<T, D>(vt16, 16 * pc, 32 * dt, lane), pf[pc], acc[dt]);
       }
       if constexpr (F32) acc[dt] += sum;  // a tile's products are added once
     }
@@ -349,8 +338,13 @@ __global__ __launch_bounds__(256, (StreamTile<T, D, RW>::OCC)) void scored_strea
   }
   while (t < t1) {
     const int tn = docs.next(t + 1, t1);
-    const bool one_doc = ids.z == 0 && docs.uniform(t);
-    const bool plain = (int64_t)(t + 1) * BK <= lim_lo && one_doc && row_last - row0 == C::ROWS - 1;
+    const bool masked = (int64_t)(t + 1) * BK > lim_lo;
+    bool by_doc = false, absent = false;
+    if (sa.q_doc) {
+      const int2 of = docs.of_tile(t);
+      by_doc = ids.z || docs.mixed(of);
+      absent = of.x < 0;
+    }
     if constexpr (F32) {
       if (tn < t1) load_stage(tn);
     } else {
@@ -359,8 +353,18 @@ __global__ __launch_bounds__(256, (StreamTile<T, D, RW>::OCC)) void scored_strea
       else wait_lds_reads();
       if (tn < t1) copy_tile(tn, buf ^ 1);
     }
-    if (plain) tile(std::false_type{}, t, buf, true);
-    else tile(std::true_type{}, t, buf, one_doc);
+    if (absent) {
+      const int* kd = sa.k_doc + (int64_t)b0 * p.n_k;
+      LE* st = reinterpret_cast<LE*>(smem + buf * C::STAGE_BYTES);
+      if constexpr (F32)
+        zero_absent<LE, D, C::RSK, C::RSV, C::TILEK, C::TILEV, C::NP>(st, st + C::NP * C::TILEK, kd, (int64_t)t * BK, lim_hi, 0, BK,
+                                                                      tid, C::NT);
+      else
+        zero_absent<LE, D, D, D, 0, 0, 1>(st, st + BK * D, kd, (int64_t)t * BK, lim_hi, OWN ? BKW * wave : 0, OWN ? BKW : BK,
+                                          OWN ? lane : tid, OWN ? 64 : C::NT);
+      if constexpr (!OWN) __syncthreads();
+    }
+    tile(t, buf, masked, by_doc);
     if constexpr (F32) {
       if (C::NBUF == 1) __syncthreads();
       if (tn < t1) store_stage(C::NBUF == 1 ? 0 : buf ^ 1);
