@@ -16,7 +16,10 @@
 // span, so only the tiles within the span of the diagonal read it element by
 // element (from LDS); the others add one value.
 //
-// Scores are kept times log2 e from the cap or the bias on (weights are 2^s).
+// Scores are kept in units of `unit` powers of two until their exponential: raw
+// products (unit = scale log2 e), or tanh (unit = cap log2 e).  Biases are divided by
+// it, so that one FMA makes the exponent whatever came before, and a bias that is
+// the same for all keys of a tile joins the row's offset in that FMA.
 #pragma once
 
 #include <type_traits>
@@ -41,7 +44,8 @@ struct ScoreArgs {
   const int* kv_len;     // [B] or null
   const int2* q_range;   // smallest and largest id of every 32 queries, [B, ceil(n_q / 32)]
   const int2* k_range;   // of every 32 keys
-  float cap2;            // cap * log2 e
+  float unit;            // powers of two of a score's unit: cap * log2 e, or scale * log2 e
+  int capped;
   float cap_in;          // scores to the argument of the cap's 2^x: 2 log2 e scale / cap
   float cap_small;       // scores to the argument of tanh: scale / cap
   int causal;
@@ -76,7 +80,6 @@ struct StreamParams {
   int split0;          // first summary of this launch
   int direct;          // 1: one range, o and lse are written; 0: summaries
   int tile_order;
-  float scale_log2;
   // The reference maximum is raised by a score that exceeds it by more than this
   // many powers of two: kRescaleSlack where only o is wanted, 0 where a backward will
   // follow.  A row's largest weight is then exactly 1 when it is rounded to 16 bits, and
@@ -171,14 +174,14 @@ struct TileCopy {
   }
 };
 
-// A value of the bias table, times log2 e.
-__device__ __forceinline__ float table_value(const ScoreArgs& s, int bucket, int head) {
+// A value of the bias table, in score units.
+__device__ __forceinline__ float table_value(const ScoreArgs& s, int bucket, int head, float per_unit) {
   const int64_t at = (int64_t)bucket * s.heads + head;
   float x;
   if (s.table_dtype == 0) x = static_cast<const float*>(s.table)[at];
   else if (s.table_dtype == 1) x = (float)static_cast<const _Float16*>(s.table)[at];
   else x = (float)static_cast<const __bf16*>(s.table)[at];
-  return x * kLog2eF;
+  return x * per_unit;
 }
 // Bucket of a side for a distance >= 0: the last one that starts at most there.
 __device__ __forceinline__ int side_bucket(const ScoreArgs& s, int distance) {
@@ -186,13 +189,18 @@ __device__ __forceinline__ int side_bucket(const ScoreArgs& s, int distance) {
   for (int e = 0; e < s.n_edges; ++e) n += s.edges[e] <= distance;
   return n - 1;
 }
-// The bias by place: place x stands for j - pos = x - span (clamped to +-span,
-// or to [-span, 0] where keys ahead count as distance 0).
+// The bias by place: place x stands for the distance j - pos = x - span - kPad.  Where
+// it is beyond the span (or ahead, with keys ahead at distance 0) the value repeats; a
+// tile of 32 x 32 pairs that is not all beyond the span stays within the kPad places
+// beyond it, so that its places are one address per lane and constant offsets.
+constexpr int kPad = 64;
+__host__ __device__ __forceinline__ int bias_ahead(const ScoreArgs& s) { return s.two_sided ? s.span : 0; }
 __host__ __device__ __forceinline__ int bias_places(const ScoreArgs& s) {
-  return s.table ? (s.two_sided ? 2 * s.span + 1 : s.span + 1) : 0;
+  return s.table ? s.span + bias_ahead(s) + 1 + 2 * kPad : 0;
 }
 __device__ __forceinline__ int place_bucket(const ScoreArgs& s, int x) {
-  const int d = x - s.span;
+  int d = x - s.span - kPad;
+  if (d > bias_ahead(s)) d = bias_ahead(s);
   return side_bucket(s, d < 0 ? -d : d) + (d > 0 ? s.n_edges : 0);
 }
 // LDS bytes of the bias for fold heads: the values by place, or (several heads)
@@ -205,14 +213,16 @@ __host__ __device__ __forceinline__ int bias_lds_bytes(const ScoreArgs& s, int f
 }
 __device__ __forceinline__ void fill_bias(const ScoreArgs& s, unsigned char* lds, int fold, int head0, int tid, int nt) {
   const int n = bias_places(s);
+  const float per_unit = kLog2eF / s.unit;
   if (fold == 1) {
-    for (int x = tid; x < n; x += nt) reinterpret_cast<float*>(lds)[x] = table_value(s, place_bucket(s, x), head0);
+    for (int x = tid; x < n; x += nt)
+      reinterpret_cast<float*>(lds)[x] = table_value(s, place_bucket(s, x), head0, per_unit);
     return;
   }
   for (int x = tid; x < n; x += nt) lds[x] = (unsigned char)place_bucket(s, x);
   const int nb = s.n_edges * (s.two_sided ? 2 : 1);
   float* tab = reinterpret_cast<float*>(lds + (n + 15) / 16 * 16);
-  for (int e = tid; e < fold * nb; e += nt) tab[e] = table_value(s, e % nb, head0 + e / nb);
+  for (int e = tid; e < fold * nb; e += nt) tab[e] = table_value(s, e % nb, head0 + e / nb, per_unit);
 }
 // The bias at a place for head g of the fold.
 __device__ __forceinline__ float bias_at(const ScoreArgs& s, const unsigned char* lds, int fold, int g, int x) {
@@ -370,7 +380,7 @@ struct ScoredBwdParams {
   int64_t n_q, n_k, n_q_pad;
   int n_b, heads_kv, heads_per_kv;
   int n_ktiles, n_qtiles, tile_order;
-  float scale, scale_log2;
+  float scale;
   TensorStrides sq, sk, sv, so, sdo, sdq, sdk, sdv;
   ScoreArgs s;
 };

@@ -57,6 +57,7 @@ ScoreArgs score_args(const mea_problem* p, const mea_score* s) {
   a.kv_len = p->kv_len;
   a.causal = p->causal;
   a.heads = (int)p->heads;
+  a.unit = p->scale * kLog2e;
   if (!s) return a;
   a.slopes = s->slopes;
   a.q_doc = s->q_doc;
@@ -64,7 +65,8 @@ ScoreArgs score_args(const mea_problem* p, const mea_score* s) {
   a.q_pos = s->q_pos;
   a.prefix = s->prefix_len;
   if (s->softcap > 0.0f) {
-    a.cap2 = s->softcap * kLog2e;
+    a.capped = 1;
+    a.unit = s->softcap * kLog2e;
     a.cap_in = 2.0f * kLog2e * p->scale / s->softcap;
     a.cap_small = p->scale / s->softcap;
   }
@@ -160,7 +162,6 @@ StreamParams stream_params(const mea_problem* p, const ScoreArgs& s, int64_t kv_
   q.groups_per_kv = q.heads_per_kv / q.fold;
   q.n_groups = (int)pl.groups;
   q.n_splits = (int)pl.splits;
-  q.scale_log2 = p->scale * kLog2e;
   q.slack = mea::kRescaleSlack;
   return q;
 }
@@ -221,7 +222,7 @@ struct PrefixWork {
 };
 PrefixWork plan_prefix(const mea_problem* p, const mea_shared_prefix* x) {
   PrefixWork w;
-  const ScoreArgs none = {};
+  const ScoreArgs none = score_args(p, nullptr);
   const int64_t kv = kv_heads_of(p, x->kv_heads);
   w.shared = plan_stream(p, none, kv, true, x->n_p);
   w.own = plan_stream(p, none, kv, false, p->n_k);
@@ -331,7 +332,6 @@ mea_status mea_scored_attention_bwd(const mea_problem* p, const mea_score* s, co
   a.heads_kv = (int)kv;
   a.heads_per_kv = (int)(p->heads / kv);
   a.scale = p->scale;
-  a.scale_log2 = p->scale * kLog2e;
   {
     const mea_strides* t = p->strides;
     const size_t e = elem_size(p->dtype);
@@ -424,8 +424,9 @@ mea_status mea_prefix_attention_fwd(const mea_problem* p, const mea_shared_prefi
   const int64_t parts = w.shared.splits + w.own.splits;
   carve_parts(&own, p, parts, align256(workspace, 0));
   own.split0 = (int)w.shared.splits;
-  StreamParams pre = stream_params(p, ScoreArgs{}, kv, w.shared);
-  pre.s.heads = (int)p->heads;
+  StreamParams pre = stream_params(p, score_args(p, nullptr), kv, w.shared);
+  pre.s.causal = 0;  // every query sees the whole prefix
+  pre.s.kv_len = nullptr;
   pre.q = q;
   pre.sq = own.sq;
   pre.k = x->k;

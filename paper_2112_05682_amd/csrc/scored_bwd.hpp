@@ -12,7 +12,7 @@
 //          registers; a key on each lane;
 //   dq   : a wave per 32 queries (Q, dO in registers) over the keys; a query on each
 //          lane.  Its dS also gives the bias gradient: per lane one sum for each
-//          side beyond the span, and within it sums by distance in LDS.
+//          side beyond the span, and within it sums of each tile's diagonals.
 #pragma once
 
 #include "scored.hpp"
@@ -73,7 +73,7 @@ struct ScoredKvTile {
   // 16-bit, d = 128: the K fragments of every lane wait in LDS (32 registers less).
   static constexpr bool K_LDS = !F32 && D == 128;
   static constexpr int KSLOT_BYTES = K_LDS ? NT * (D / 16) * 16 : 0;
-  static constexpr int kBiasMax = 4 * (2 * kMaxBiasSpan + 1) + 16;
+  static constexpr int kBiasMax = 4 * (2 * kMaxBiasSpan + 1 + 2 * kPad) + 16;
   static constexpr int NBUF = 2 * STAGE_BYTES + KSLOT_BYTES + kBiasMax <= 160 * 1024 / OCC - 64 ? 2 : 1;
   static constexpr int LDS_BYTES = NBUF * STAGE_BYTES + KSLOT_BYTES;
   static constexpr int CPR = D / 8, CHUNKS = 2 * BQ * CPR, CPT = CHUNKS / NT;
@@ -85,7 +85,7 @@ template <typename T, int D, bool CAP, bool BIAS>
 __global__ __launch_bounds__(256, (ScoredKvTile<T, D>::OCC)) void scored_dkdv_kernel(ScoredBwdParams p) {
   using C = ScoredKvTile<T, D>;
   using LE = typename Planes<T>::E;
-  constexpr bool F32 = C::F32, LOG2 = CAP || BIAS;
+  constexpr bool F32 = C::F32;
   constexpr int BQ = C::BQ, QS = C::QS, KC = D / 16, NDT = D / 32, NBUF = C::NBUF;
 
   extern __shared__ __align__(16) unsigned char smem[];
@@ -219,8 +219,8 @@ __global__ __launch_bounds__(256, (ScoredKvTile<T, D>::OCC)) void scored_dkdv_ke
   };
 
   const int qrow = perm32(c);
-  const float cl2 = p.scale_log2;
-  float slope2 = 0.0f;
+  const float unit = sa.unit;
+  float slope = 0.0f;
 
   // One tile of queries: masked, some query sees some key of the workgroup not; by_doc,
   // documents differ (uniform branches of one copy of the code, as in the forward).
@@ -269,40 +269,38 @@ __global__ __launch_bounds__(256, (ScoredKvTile<T, D>::OCC)) void scored_dkdv_ke
         }
       }
       float grad[CAP ? 16 : 1];  // 1 - tanh^2
-      if constexpr (LOG2) {
+      if constexpr (CAP) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          if constexpr (CAP) {
-            const float th = cap_tanh<T>(sa, s[r]);
-            grad[r] = fmaf(-th, th, 1.0f);
-            s[r] = sa.cap2 * th;
-          } else {
-            s[r] *= cl2;
-          }
+          s[r] = cap_tanh<T>(sa, s[r]);
+          grad[r] = fmaf(-s[r], s[r], 1.0f);
         }
       }
+      float add = 0.0f;  // what every pair gets
       if constexpr (BIAS) {
         const int off = (int)key - (int)(pos0 + q0) - 8 * h;  // distance to the tile's first query, less 8 h
+        const int64_t p_lo = pos0 + q0, p_hi = p_lo + 31;
         if (sa.slopes) {
-          const float d0 = (float)off;
+          if (kw + 31 <= p_lo) {
+            add = (float)off * slope;
 #pragma unroll
-          for (int r = 0; r < 16; ++r) s[r] = fmaf(-fabsf(d0 - (float)permuted_row(r, 0)), slope2, s[r]);
-        }
-        if (sa.table) {
-          const int hi = sa.two_sided ? sa.span : 0, last = bias_places(sa) - 1;
-          const int64_t p_lo = pos0 + q0, p_hi = p_lo + 31;
-          if (kw + 31 <= p_lo - sa.span || kw >= p_hi + hi) {
-            const float x = reinterpret_cast<const float*>(lds_bias)[kw >= p_hi + hi ? last : 0];
-#pragma unroll
-            for (int r = 0; r < 16; ++r) s[r] += x;
+            for (int r = 0; r < 16; ++r) s[r] = fmaf((float)permuted_row(r, 0), -slope, s[r]);
           } else {
             asm volatile("");
+            const float d0 = (float)off;
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-              int d = off - permuted_row(r, 0);
-              d = d < -sa.span ? -sa.span : (d > hi ? hi : d);
-              s[r] += reinterpret_cast<const float*>(lds_bias)[d + sa.span];
-            }
+            for (int r = 0; r < 16; ++r) s[r] = fmaf(-fabsf(d0 - (float)permuted_row(r, 0)), slope, s[r]);
+          }
+        }
+        if (sa.table) {
+          const int hi = bias_ahead(sa);
+          if (kw + 31 <= p_lo - sa.span || kw >= p_hi + hi) {
+            add += reinterpret_cast<const float*>(lds_bias)[kw >= p_hi + hi ? bias_places(sa) - 1 : 0];
+          } else {
+            asm volatile("");
+            const float* at = reinterpret_cast<const float*>(lds_bias) + (off + sa.span + kPad);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[r] += at[-permuted_row(r, 0)];
           }
         }
       }
@@ -333,7 +331,7 @@ __global__ __launch_bounds__(256, (ScoredKvTile<T, D>::OCC)) void scored_dkdv_ke
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const int r = 8 * m + 4 * j + e;
-            x[4 * j + e] = fast_exp2(LOG2 ? s[r] - l2[e] : fmaf(s[r], cl2, -l2[e]));
+            x[4 * j + e] = fast_exp2(fmaf(s[r], unit, BIAS ? fmaf(add, unit, -l2[e]) : -l2[e]));
             y[4 * j + e] = x[4 * j + e] * dp[r];
             if constexpr (CAP) y[4 * j + e] *= grad[r];
           }
@@ -386,7 +384,7 @@ __global__ __launch_bounds__(256, (ScoredKvTile<T, D>::OCC)) void scored_dkdv_ke
     }
     if constexpr (BIAS) {
       if (g != g_bias) {  // the heads' biases take turns
-        if (sa.slopes) slope2 = sa.slopes[head_of(g)] * kLog2eF;
+        if (sa.slopes) slope = sa.slopes[head_of(g)] * (kLog2eF / unit);
         if (sa.table) {
           fill_bias(sa, lds_bias, 1, head_of(g), tid, C::NT);
           __syncthreads();
@@ -452,24 +450,20 @@ struct ScoredDqTile {
   static constexpr int TILE_BYTES = F32 ? NP * TILE * 2 : BK * D * 2;
   static constexpr int STAGE_BYTES = 2 * TILE_BYTES;
   static constexpr int OCC = F32 && D == 128 ? 1 : 2;
-  // The bias by place and, for its gradient, sums by place of each wave and half.
-  static constexpr int kBiasMax = 4 * (2 * kMaxBiasSpan + 1) + 16;
-  static constexpr int NBUF = 2 * STAGE_BYTES + 9 * kBiasMax <= 160 * 1024 / OCC - 256 ? 2 : 1;
+  // The bias by place; its gradient takes 4 waves' sums by place and 32 KiB more.
+  static constexpr int kBiasMax = 4 * (2 * kMaxBiasSpan + 1 + 2 * kPad) + 16;
+  static constexpr int NBUF = 2 * STAGE_BYTES + 5 * kBiasMax + 32768 <= 160 * 1024 - 256 ? 2 : 1;
   static constexpr int LDS_BYTES = NBUF * STAGE_BYTES;
   static constexpr int CPR = D / 8, CHUNKS = 2 * BK * CPR, CPT = CHUNKS / NT;
   static_assert(CHUNKS % NT == 0, "tile shapes");
   static_assert(F32 || NBUF == 2, "asynchronous copies need two stages");
 };
 
-__device__ __forceinline__ void lds_add(float* p, float x) {
-  __hip_atomic_fetch_add(p, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
-}
-
 template <typename T, int D, bool CAP, bool BIAS>
 __global__ __launch_bounds__(256, (ScoredDqTile<T, D>::OCC)) void scored_dq_kernel(ScoredBwdParams p) {
   using C = ScoredDqTile<T, D>;
   using LE = typename Planes<T>::E;
-  constexpr bool F32 = C::F32, LOG2 = CAP || BIAS;
+  constexpr bool F32 = C::F32;
   constexpr int BK = C::BK, KC = D / 16, NKT = BK / 32, NDT = D / 32, NBUF = C::NBUF;
 
   extern __shared__ __align__(16) unsigned char smem[];
@@ -514,17 +508,20 @@ __global__ __launch_bounds__(256, (ScoredDqTile<T, D>::OCC)) void scored_dq_kern
   const int n_units = (int)((p.n_k + 31) / 32);
   DocTiles<BK / 32> docs(sa.k_range ? sa.k_range + (int64_t)b * n_units : nullptr, n_units, ids.x, ids.y);
 
-  const float slope2 = BIAS && sa.slopes ? sa.slopes[head] * kLog2eF : 0.0f;
+  const float unit = sa.unit;
+  const float slope = BIAS && sa.slopes ? sa.slopes[head] * (kLog2eF / unit) : 0.0f;
   const int places = BIAS ? bias_places(sa) : 0;
   const bool sums = BIAS && p.table_part;
-  // Sums by place, of each wave and lane half (their lanes of one instruction have
-  // places of their own, so that the order of the additions is fixed).
+  // For the bias gradient: sums by place of each wave, and each wave's 32 x 64 skewed
+  // tile: dS of row c and key x at column x - c + 31, so that a column is a diagonal;
+  // the places that no pair has stay 0.
   float* const bins = reinterpret_cast<float*>(lds_bias + bias_lds_bytes(sa, 1));
-  float* const my_bins = bins + (2 * wave + h) * places;
+  float* const my_bins = bins + wave * places;
+  float* const skew = bins + 4 * places + 2048 * wave;
   if (BIAS && sa.table) {
     fill_bias(sa, lds_bias, 1, head, tid, C::NT);
     if (sums)
-      for (int x = tid; x < 8 * places; x += C::NT) bins[x] = 0.0f;
+      for (int x = tid; x < 4 * places + 8192; x += C::NT) bins[x] = 0.0f;
   }
 
   const T* __restrict__ kg = static_cast<const T*>(p.k) + (int64_t)b * p.sk.b + (int64_t)kvh * p.sk.h;
@@ -586,7 +583,6 @@ __global__ __launch_bounds__(256, (ScoredDqTile<T, D>::OCC)) void scored_dq_kern
   };
 
   const int krow = perm32(c);
-  const float cl2 = p.scale_log2;
   const int64_t p_lo = pos0 + qw, p_hi = pos0 + w_last;  // the wave's positions
 
   auto tile = [&](int t, int buf, bool masked, bool by_doc) __attribute__((always_inline)) {
@@ -627,40 +623,38 @@ __global__ __launch_bounds__(256, (ScoredDqTile<T, D>::OCC)) void scored_dq_kern
         }
       }
       float grad[CAP ? 16 : 1];
-      if constexpr (LOG2) {
+      if constexpr (CAP) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          if constexpr (CAP) {
-            const float th = cap_tanh<T>(sa, s[r]);
-            grad[r] = fmaf(-th, th, 1.0f);
-            s[r] = sa.cap2 * th;
-          } else {
-            s[r] *= cl2;
-          }
+          s[r] = cap_tanh<T>(sa, s[r]);
+          grad[r] = fmaf(-s[r], s[r], 1.0f);
         }
       }
-      const int off = BIAS ? (int)k0 - pos + 8 * h : 0;
-      const int hi = sa.two_sided ? sa.span : 0;
+      float add = 0.0f;  // what every pair gets
+      const int off = BIAS ? (int)k0 - pos + 8 * h : 0;  // distance of the lane's first key
+      const int hi = bias_ahead(sa);
       const bool far = BIAS && (k0 + 31 <= p_lo - sa.span || k0 >= p_hi + hi);
       if constexpr (BIAS) {
         if (sa.slopes) {
-          const float d0 = (float)off;
+          if (k0 + 31 <= p_lo) {
+            add = (float)off * slope;
 #pragma unroll
-          for (int r = 0; r < 16; ++r) s[r] = fmaf(-fabsf(d0 + (float)permuted_row(r, 0)), slope2, s[r]);
+            for (int r = 0; r < 16; ++r) s[r] = fmaf((float)permuted_row(r, 0), slope, s[r]);
+          } else {
+            asm volatile("");
+            const float d0 = (float)off;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[r] = fmaf(-fabsf(d0 + (float)permuted_row(r, 0)), slope, s[r]);
+          }
         }
         if (sa.table) {
           if (far) {
-            const float x = reinterpret_cast<const float*>(lds_bias)[k0 >= p_hi + hi ? places - 1 : 0];
-#pragma unroll
-            for (int r = 0; r < 16; ++r) s[r] += x;
+            add += reinterpret_cast<const float*>(lds_bias)[k0 >= p_hi + hi ? places - 1 : 0];
           } else {
             asm volatile("");
+            const float* at = reinterpret_cast<const float*>(lds_bias) + (off + sa.span + kPad);
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-              int d = off + permuted_row(r, 0);
-              d = d < -sa.span ? -sa.span : (d > hi ? hi : d);
-              s[r] += reinterpret_cast<const float*>(lds_bias)[d + sa.span];
-            }
+            for (int r = 0; r < 16; ++r) s[r] += at[permuted_row(r, 0)];
           }
         }
       }
@@ -680,8 +674,9 @@ __global__ __launch_bounds__(256, (ScoredDqTile<T, D>::OCC)) void scored_dq_kern
           if (id != doc) s[r] = -INFINITY;
         }
       }
+      const float neg = BIAS ? fmaf(add, unit, -l2) : -l2;
 #pragma unroll
-      for (int r = 0; r < 16; ++r) dp[r] *= fast_exp2(LOG2 ? s[r] - l2 : fmaf(s[r], cl2, -l2));  // dS
+      for (int r = 0; r < 16; ++r) dp[r] *= fast_exp2(fmaf(s[r], unit, neg));  // dS
       if constexpr (BIAS) {
         if (sums) {
           if (far) {
@@ -693,13 +688,15 @@ __global__ __launch_bounds__(256, (ScoredDqTile<T, D>::OCC)) void scored_dq_kern
             else far_lo += x;
           } else {
             asm volatile("");
+            // A lane adds a diagonal of the wave's tile.  (LDS atomics by distance took 166
+            // cycles an instruction; this takes 48 reads and writes for 16 of them.)
+            float* const to = skew + 63 * c + 31 + 8 * h;
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-              const int d = off + permuted_row(r, 0);
-              if (d <= -sa.span) far_lo += dp[r];
-              else if (d >= hi) far_hi += dp[r];
-              else lds_add(my_bins + d + sa.span, dp[r]);
-            }
+            for (int r = 0; r < 16; ++r) to[permuted_row(r, 0)] = dp[r];
+            float y[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int x = 0; x < 32; ++x) y[x & 3] += skew[64 * x + lane];
+            my_bins[(int)(k0 - p_lo) + lane - 31 + sa.span + kPad] += (y[0] + y[1]) + (y[2] + y[3]);
           }
         }
       }
@@ -784,8 +781,9 @@ __global__ __launch_bounds__(256, (ScoredDqTile<T, D>::OCC)) void scored_dq_kern
 
   if constexpr (BIAS) {
     if (!sums) return;
-    // The workgroup's sums by bucket: waves and halves in order, then a bucket's places
-    // in order, the ends beyond the span with the far sums.
+    // The workgroup's sums by bucket: by place over the waves in order, then
+    // a bucket's places in order.  Places beyond the span belong to the last bucket of
+    // their side, as do the far sums (with keys ahead at distance 0: to bucket 0).
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) {
       far_lo += __shfl_xor(far_lo, o);
@@ -799,23 +797,30 @@ __global__ __launch_bounds__(256, (ScoredDqTile<T, D>::OCC)) void scored_dq_kern
     for (int x = tid; x < places; x += C::NT) {
       float y = bins[x];
 #pragma unroll
-      for (int w = 1; w < 8; ++w) y += bins[w * places + x];
+      for (int w = 1; w < 4; ++w) y += bins[w * places + x];
       if (x == 0) y += (far_sums[0] + far_sums[1]) + (far_sums[2] + far_sums[3]);
       if (x == places - 1) y += (far_sums[4] + far_sums[5]) + (far_sums[6] + far_sums[7]);
       bins[x] = y;
     }
     __syncthreads();
-    const int nb = sa.n_edges * (sa.two_sided ? 2 : 1);
+    const int nb = sa.n_edges * (sa.two_sided ? 2 : 1), zero = sa.span + kPad;  // place of distance 0
     // Workgroups of one head are neighbours in table_part: [head][batch][query tile].
     float* part = p.table_part + (((int64_t)head * p.n_b + b) * p.n_qtiles + qtile) * nb;
     for (int e = tid; e < nb; e += C::NT) {
       const bool ahead = e >= sa.n_edges;
       const int s = ahead ? e - sa.n_edges : e;
-      int lo = sa.edges[s], end = s + 1 < sa.n_edges ? sa.edges[s + 1] : sa.span + 1;  // distances [lo, end)
-      if (end > sa.span + 1) end = sa.span + 1;
-      if (ahead && lo == 0) lo = 1;  // distance 0 is behind
+      // Its places [lo, end).
+      int lo = s + 1 < sa.n_edges ? sa.edges[s] : sa.span, end = s + 1 < sa.n_edges ? sa.edges[s + 1] : sa.span + 1 + kPad;
+      if (ahead) {
+        lo = zero + (lo > 0 ? lo : 1);  // distance 0 is behind
+        end = zero + end;
+      } else {
+        const int from = zero - end + 1;
+        end = s == 0 && !sa.two_sided ? places : zero - lo + 1;
+        lo = from;
+      }
       float y = 0.0f;
-      for (int d = lo; d < end; ++d) y += bins[sa.span + (ahead ? d : -d)];
+      for (int x = lo; x < end; ++x) y += bins[x];
       part[e] = y;
     }
   }
@@ -839,7 +844,7 @@ static hipError_t launch_scored_bwd_kernels(const ScoredBwdParams& p, hipStream_
     if (e != hipSuccess) return e;
   }
   if (!p.dq) return e;
-  const int bins = p.table_part ? 8 * bias_places(p.s) * 4 : 0;
+  const int bins = p.table_part ? (4 * bias_places(p.s) + 8192) * 4 : 0;
   e = hipLaunchKernel(reinterpret_cast<const void*>(scored_dq_kernel<T, D, CAP, BIAS>),
                       dim3((unsigned)((int64_t)a.n_qtiles * p.n_b * p.s.heads)), dim3(Q::NT), args,
                       Q::LDS_BYTES + bias + bins, stream);
@@ -855,7 +860,7 @@ static hipError_t launch_scored_bwd_d(const ScoredBwdParams& p, hipStream_t stre
   const hipError_t e = hipLaunchKernel(reinterpret_cast<const void*>(scored_bwd_pre_kernel<T, D>),
                                        dim3((unsigned)((rows + RPB - 1) / RPB)), dim3(256), args, 0, stream);
   if (e != hipSuccess) return e;
-  const bool cap = p.s.cap2 != 0.0f, bias = p.s.slopes || p.s.table;
+  const bool cap = p.s.capped, bias = p.s.slopes || p.s.table;
   if (cap)
     return bias ? launch_scored_bwd_kernels<T, D, true, true>(p, stream)
                 : launch_scored_bwd_kernels<T, D, true, false>(p, stream);

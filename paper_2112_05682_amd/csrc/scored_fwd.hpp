@@ -26,7 +26,7 @@ struct StreamTile {
   static constexpr int STAGE_BYTES = F32 ? NP * (TILEK + TILEV) * 2 : 2 * BK * D * 2;
   // Workgroups per CU that the registers are kept to.
   static constexpr int OCC = F32 ? (D == 64 && RW == 4 ? 2 : 1) : (RW == 1 ? (D == 64 ? 2 : 1) : (D == 64 ? 3 : 2));
-  static constexpr int kBiasMax = 4 * (2 * kMaxBiasSpan + 1) + 16;
+  static constexpr int kBiasMax = 4 * (2 * kMaxBiasSpan + 1 + 2 * kPad) + 16;
   static constexpr int NBUF = 2 * STAGE_BYTES + kBiasMax <= 160 * 1024 / OCC ? 2 : 1;
   static constexpr int ML_BYTES = 2 * 4 * 32 * 4;
   static constexpr int RED_BYTES = KW > 1 ? ML_BYTES + RW * (D / 32) * (KW - 1) * 4096 : 0;
@@ -44,8 +44,6 @@ __global__ __launch_bounds__(256, (StreamTile<T, D, RW>::OCC)) void scored_strea
   using LE = typename Planes<T>::E;
   constexpr bool F32 = C::F32;
   constexpr int KW = C::KW, BK = C::BK, BKW = C::BKW, KC = D / 16, NKT = BKW / 32, NPC = BKW / 16, NDT = D / 32;
-  // Whether scores hold 2^s exponents (else raw products, times scale log2 e later).
-  constexpr bool LOG2 = CAP || BIAS;
 
   extern __shared__ __align__(16) unsigned char smem[];
   unsigned char* const lds_bias = smem + C::LDS_BYTES;
@@ -108,7 +106,8 @@ __global__ __launch_bounds__(256, (StreamTile<T, D, RW>::OCC)) void scored_strea
   const int n_units = (int)((p.n_k + 31) / 32);
   DocTiles<UNITS> docs(sa.k_range ? sa.k_range + (int64_t)b0 * n_units : nullptr, n_units, ids.x, ids.y);
 
-  const float slope2 = BIAS && sa.slopes ? sa.slopes[head] * kLog2eF : 0.0f;
+  const float unit = sa.unit;
+  const float slope = BIAS && sa.slopes ? sa.slopes[head] * (kLog2eF / unit) : 0.0f;
   if (BIAS && sa.table) fill_bias(sa, lds_bias, p.fold, head0, tid, C::NT);
 
   // ---- keys of this range: the visible tiles dealt evenly.
@@ -180,7 +179,6 @@ __global__ __launch_bounds__(256, (StreamTile<T, D, RW>::OCC)) void scored_strea
   };
 
   const int krow = perm32(c);
-  const float cl2 = p.scale_log2;
 
   // One tile: masked, some key is beyond some row's limit; by_doc, documents differ.
   // The masks are uniform branches (an empty volatile statement each, so that they do
@@ -217,38 +215,53 @@ __global__ __launch_bounds__(256, (StreamTile<T, D, RW>::OCC)) void scored_strea
 #pragma unroll
       for (int kt = 0; kt < NKT; ++kt) s[kt] += rest[kt];
 
-    // Cap and bias.
-    if constexpr (LOG2) {
+    // Cap and bias.  add: what every key of the tile gets.
+    if constexpr (CAP) {
 #pragma unroll
       for (int kt = 0; kt < NKT; ++kt)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) s[kt][r] = CAP ? sa.cap2 * cap_tanh<T>(sa, s[kt][r]) : s[kt][r] * cl2;
+        for (int r = 0; r < 16; ++r) s[kt][r] = cap_tanh<T>(sa, s[kt][r]);
     }
+    float add = 0.0f;
     if constexpr (BIAS) {
-      const int off = (int)k0 - pos;  // first key's distance
+      const int off = (int)k0 - pos + 8 * h;  // distance of the lane's first key
       if (sa.slopes) {
-        const float d0 = (float)(off + 8 * h);
+        if (k0 + BKW - 1 <= wq_lo) {  // no key is ahead: -|d| = d
+          add = (float)off * slope;
 #pragma unroll
-        for (int kt = 0; kt < NKT; ++kt)
+          for (int kt = 0; kt < NKT; ++kt)
 #pragma unroll
-          for (int r = 0; r < 16; ++r) s[kt][r] = fmaf(-fabsf(d0 + (float)(32 * kt + permuted_row(r, 0))), slope2, s[kt][r]);
+            for (int r = 0; r < 16; ++r) s[kt][r] = fmaf((float)(32 * kt + permuted_row(r, 0)), slope, s[kt][r]);
+        } else {
+          asm volatile("");
+          const float d0 = (float)off;
+#pragma unroll
+          for (int kt = 0; kt < NKT; ++kt)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[kt][r] = fmaf(-fabsf(d0 + (float)(32 * kt + permuted_row(r, 0))), slope, s[kt][r]);
+        }
       }
       if (sa.table) {
-        const int hi = sa.two_sided ? sa.span : 0, last = bias_places(sa) - 1;
+        const int hi = bias_ahead(sa), last = bias_places(sa) - 1;
+        if (k0 + BKW - 1 <= wq_lo - sa.span || k0 >= wq_hi + hi) {  // one value for every key of a row
+          add += bias_at(sa, lds_bias, p.fold, g, k0 >= wq_hi + hi ? last : 0);
+        } else {
+          asm volatile("");
 #pragma unroll
-        for (int kt = 0; kt < NKT; ++kt) {
-          const int64_t ka = k0 + 32 * kt;
-          if (ka + 31 <= wq_lo - sa.span || ka >= wq_hi + hi) {  // one value for every key of a row
-            const float v = bias_at(sa, lds_bias, p.fold, g, ka >= wq_hi + hi ? last : 0);
+          for (int kt = 0; kt < NKT; ++kt) {
+            const int64_t ka = k0 + 32 * kt;
+            if (ka + 31 <= wq_lo - sa.span || ka >= wq_hi + hi) {
+              const float v = bias_at(sa, lds_bias, p.fold, g, ka >= wq_hi + hi ? last : 0);
 #pragma unroll
-            for (int r = 0; r < 16; ++r) s[kt][r] += v;
-          } else {
-            asm volatile("");
+              for (int r = 0; r < 16; ++r) s[kt][r] += v;
+            } else if (p.fold == 1) {
+              const float* at = reinterpret_cast<const float*>(lds_bias) + (off + 32 * kt + sa.span + kPad);
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-              int d = off + 32 * kt + permuted_row(r, h);
-              d = d < -sa.span ? -sa.span : (d > hi ? hi : d);
-              s[kt][r] += bias_at(sa, lds_bias, p.fold, g, d + sa.span);
+              for (int r = 0; r < 16; ++r) s[kt][r] += at[permuted_row(r, 0)];
+            } else {
+#pragma unroll
+              for (int r = 0; r < 16; ++r)
+                s[kt][r] += bias_at(sa, lds_bias, p.fold, g, off + 32 * kt + permuted_row(r, 0) + sa.span + kPad);
             }
           }
         }
@@ -285,8 +298,7 @@ __global__ __launch_bounds__(256, (StreamTile<T, D, RW>::OCC)) void scored_strea
     for (int kt = 0; kt < NKT; ++kt)
 #pragma unroll
       for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[kt][r]);
-    const float mul = LOG2 ? 1.0f : cl2;
-    const float mx_c = xhalf_max(mx) * mul;
+    const float mx_c = xhalf_max(mx + add) * unit;  // (the halves' add differs with slopes)
     const bool raise = mx_c > m_ref + p.slack;
     if (__builtin_amdgcn_ballot_w64(raise)) {
       const float m_new = raise ? mx_c : m_ref;
@@ -299,16 +311,13 @@ __global__ __launch_bounds__(256, (StreamTile<T, D, RW>::OCC)) void scored_strea
       m_ref = m_new;
     }
     // A row with no visible key so far: its (all -inf) exponents get weight 0.
-    const float neg = m_ref == -INFINITY ? 0.0f : -m_ref;
+    const float neg = m_ref == -INFINITY ? 0.0f : fmaf(add, unit, -m_ref);
     Frag<T> pf[NPC];
 #pragma unroll
     for (int pc = 0; pc < NPC; ++pc) {
       float e8[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float v = s[pc >> 1][8 * (pc & 1) + e];
-        e8[e] = fast_exp2(LOG2 ? v + neg : fmaf(v, cl2, neg));
-      }
+      for (int e = 0; e < 8; ++e) e8[e] = fast_exp2(fmaf(s[pc >> 1][8 * (pc & 1) + e], unit, neg));
       pf[pc] = to_frag<T>(e8);
       l_run = tree_sum<8>(e8, l_run);
     }
@@ -522,7 +531,7 @@ static hipError_t launch_stream_kernel(const StreamParams& p, hipStream_t stream
 }
 template <typename T, int D, int RW>
 static hipError_t launch_stream_mods(const StreamParams& p, hipStream_t stream) {
-  const bool cap = p.s.cap2 != 0.0f, bias = p.s.slopes || p.s.table;
+  const bool cap = p.s.capped, bias = p.s.slopes || p.s.table;
   if (cap)
     return bias ? launch_stream_kernel<T, D, RW, true, true>(p, stream)
                 : launch_stream_kernel<T, D, RW, true, false>(p, stream);
