@@ -157,6 +157,10 @@ _native = None
 # The entry points that the extension calls, in the order of its init.
 NATIVE_CALLS = ("mea_attention_fwd_workspace_size", "mea_attention_bwd_workspace_size", "mea_attention_fwd",
                 "mea_attention_bwd")
+# Those of its init_scored.
+NATIVE_SCORED_CALLS = ("mea_scored_attention_fwd_workspace_size", "mea_scored_attention_bwd_workspace_size",
+                       "mea_scored_attention_fwd", "mea_scored_attention_bwd",
+                       "mea_prefix_attention_fwd_workspace_size", "mea_prefix_attention_fwd")
 
 
 def native():
@@ -171,6 +175,7 @@ def native():
         ext = importlib.util.module_from_spec(importlib.util.spec_from_loader(loader.name, loader))
         loader.exec_module(ext)
         ext.init(check, *(ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in NATIVE_CALLS))
+        ext.init_scored(*(ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in NATIVE_SCORED_CALLS))
         _native = ext
     return _native
 

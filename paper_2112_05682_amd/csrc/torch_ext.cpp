@@ -30,6 +30,12 @@ decltype(&mea_attention_fwd_workspace_size) g_fwd_ws;
 decltype(&mea_attention_bwd_workspace_size) g_bwd_ws;
 decltype(&mea_attention_fwd) g_fwd;
 decltype(&mea_attention_bwd) g_bwd;
+decltype(&mea_scored_attention_fwd_workspace_size) g_scored_fwd_ws;
+decltype(&mea_scored_attention_bwd_workspace_size) g_scored_bwd_ws;
+decltype(&mea_scored_attention_fwd) g_scored_fwd;
+decltype(&mea_scored_attention_bwd) g_scored_bwd;
+decltype(&mea_prefix_attention_fwd_workspace_size) g_prefix_ws;
+decltype(&mea_prefix_attention_fwd) g_prefix_fwd;
 PyObject* g_check;  // check(name, status): raises what a status means
 
 // A plain torch.Tensor or Parameter with storage on a GPU (no subclass, no
@@ -368,6 +374,290 @@ PyObject* ext_packed_bwd(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   END_HANDLE_TH_ERRORS
 }
 
+// ---- attention with modified scores and over a shared prefix
+
+// None, or a contiguous tensor of a type and shape on a device: its address in *out.
+bool vector_ok(PyObject* o, const at::Device& dev, at::ScalarType type, at::IntArrayRef shape, const void** out) {
+  *out = nullptr;
+  if (o == Py_None) return true;
+  const at::Tensor* t = gpu_tensor(o);
+  if (!t || t->scalar_type() != type || t->device() != dev || t->sizes() != shape || !t->is_contiguous()) return false;
+  *out = t->const_data_ptr();
+  return true;
+}
+
+// Shapes of q, k, v with grouped key heads.
+bool grouped_shapes(const at::Tensor& q, const at::Tensor& k, const at::Tensor& v) {
+  return q.size(0) == k.size(0) && q.size(3) == k.size(3) && k.sizes() == v.sizes() && k.size(1) > 0 &&
+         q.size(1) % k.size(1) == 0;
+}
+
+// softcap, slopes, bias, edges (None, or (address, number, two-sided)), q_doc,
+// k_doc, prefix_len, q_pos: a[0] .. a[7].  *bias: the bias or null.
+bool score(mea_score* s, PyObject* const* a, const at::Tensor& q, const at::Tensor& k, const at::Tensor** bias) {
+  *s = mea_score{};
+  *bias = nullptr;
+  const at::Device dev = q.device();
+  const int64_t B = q.size(0), H = q.size(1);
+  s->kv_heads = k.size(1);
+  if (a[0] != Py_None) {
+    const double cap = PyFloat_AsDouble(a[0]);
+    if (PyErr_Occurred()) {
+      PyErr_Clear();
+      return false;
+    }
+    s->softcap = (float)cap;
+    if (!(s->softcap > 0.0f)) return false;
+  }
+  const void* p;
+  if (!vector_ok(a[1], dev, at::kFloat, {H}, &p)) return false;
+  s->slopes = static_cast<const float*>(p);
+  if (a[2] != Py_None) {
+    const at::Tensor* t = gpu_tensor(a[2]);
+    if (!t || !PyTuple_CheckExact(a[3]) || PyTuple_GET_SIZE(a[3]) != 3) return false;
+    s->edges = static_cast<const int32_t*>(PyLong_AsVoidPtr(PyTuple_GET_ITEM(a[3], 0)));
+    s->n_edges = (int32_t)PyLong_AsLong(PyTuple_GET_ITEM(a[3], 1));
+    s->two_sided = PyObject_IsTrue(PyTuple_GET_ITEM(a[3], 2));
+    if (PyErr_Occurred()) {
+      PyErr_Clear();
+      return false;
+    }
+    if (t->device() != dev || (t->scalar_type() != at::kFloat && t->scalar_type() != q.scalar_type()) || t->dim() != 2 ||
+        t->size(1) != H || t->size(0) != (int64_t)s->n_edges * (s->two_sided ? 2 : 1) || !t->is_contiguous())
+      return false;
+    s->table = t->const_data_ptr();
+    s->table_dtype = dtype_code(t->scalar_type());
+    *bias = t;
+  }
+  if (!vector_ok(a[4], dev, at::kInt, {B, q.size(2)}, &p)) return false;
+  s->q_doc = static_cast<const int32_t*>(p);
+  if (!vector_ok(a[5], dev, at::kInt, {B, k.size(2)}, &p)) return false;
+  s->k_doc = static_cast<const int32_t*>(p);
+  if (!vector_ok(a[6], dev, at::kInt, {B}, &p)) return false;
+  s->prefix_len = static_cast<const int32_t*>(p);
+  if (!vector_ok(a[7], dev, at::kInt, {B}, &p)) return false;
+  s->q_pos = static_cast<const int32_t*>(p);
+  return true;
+}
+
+// scored_fwd(q, k, v, causal, scale, need_lse, out, kv_len, residual, <score>):
+// attention_scored_fwd's result, or None.
+PyObject* ext_scored_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  if (n != 17) return none();
+  const at::Tensor *q = gpu_tensor(a[0]), *k = gpu_tensor(a[1]), *v = gpu_tensor(a[2]), *bias;
+  if (!q || !k || !v) return none();
+  const at::ScalarType dt = q->scalar_type();
+  if (dtype_code(dt) < 0 || !in_place(*q) || !like(*k, *q, dt) || !like(*v, *q, dt) || !grouped_shapes(*q, *k, *v))
+    return none();
+  const at::Tensor* out = nullptr;
+  if (a[6] != Py_None) {
+    out = gpu_tensor(a[6]);
+    if (!out || !like(*out, *q, dt) || out->sizes() != q->sizes()) return none();
+  }
+  const int need_lse = PyObject_IsTrue(a[5]), residual = PyObject_IsTrue(a[8]);
+  mea_problem p;
+  mea_score s;
+  if (need_lse < 0 || residual < 0 ||
+      !problem(&p, q->size(0), q->size(1), q->size(2), k->size(2), q->size(3), q->size(3), dtype_code(dt), a[3], a[4], a[7],
+               q->device(), false) ||
+      !score(&s, a + 9, *q, *k, &bias)) {
+    PyErr_Clear();
+    return none();
+  }
+  at::Tensor o, lse, o_lo;
+  mea_status st;
+  {
+    pybind11::gil_scoped_release no_gil;
+    const auto opts = at::TensorOptions().dtype(dt).device(q->device());
+    size_t bytes = 0;
+    st = g_scored_fwd_ws(&p, &s, &bytes);
+    if (st == MEA_OK) {
+      o = out ? *out : at::empty(q->sizes(), opts);
+      mea_strides ms = {};
+      if (!q->is_contiguous() || !k->is_contiguous() || !v->is_contiguous() || !o.is_contiguous()) {
+        ms.q = strides_of(*q);
+        ms.k = strides_of(*k);
+        ms.v = strides_of(*v);
+        ms.o = strides_of(o);
+        p.strides = &ms;
+      }
+      if (need_lse) lse = at::empty(q->sizes().slice(0, 3), at::TensorOptions().dtype(at::kFloat).device(q->device()));
+      if (residual && dt != at::kFloat) o_lo = at::empty(q->sizes(), opts);
+      at::Tensor ws;
+      if (bytes) ws = workspace(bytes, q->device());
+      st = g_scored_fwd(&p, &s, q->const_data_ptr(), k->const_data_ptr(), v->const_data_ptr(), o.mutable_data_ptr(),
+                        lse.defined() ? static_cast<float*>(lse.mutable_data_ptr()) : nullptr,
+                        o_lo.defined() ? o_lo.mutable_data_ptr() : nullptr, bytes ? ws.mutable_data_ptr() : nullptr, bytes,
+                        stream_of(q->device()));
+    }
+  }
+  if (st != MEA_OK) return failed("mea_scored_attention_fwd", st);
+  return residual ? tuple_of({o, lse, o_lo}) : tuple_of({o, lse});
+  END_HANDLE_TH_ERRORS
+}
+
+// scored_bwd(q, k, v, o, lse, do, causal, scale, need_dq, need_dkdv, need_dbias,
+// kv_len, o_lo, <score>): attention_scored_bwd's result, or None.
+PyObject* ext_scored_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  if (n != 21) return none();
+  const at::Tensor *q = gpu_tensor(a[0]), *k = gpu_tensor(a[1]), *v = gpu_tensor(a[2]), *o = gpu_tensor(a[3]),
+                   *lse = gpu_tensor(a[4]), *d_o = gpu_tensor(a[5]), *bias;
+  if (!q || !k || !v || !o || !lse || !d_o) return none();
+  const at::ScalarType dt = q->scalar_type();
+  if (dtype_code(dt) < 0 || !in_place(*q) || !like(*k, *q, dt) || !like(*v, *q, dt) || !like(*o, *q, dt) ||
+      !like(*d_o, *q, dt) || !grouped_shapes(*q, *k, *v) || o->sizes() != q->sizes() || d_o->sizes() != q->sizes() ||
+      !lse_ok(lse, q->device(), q->size(0), q->size(1), q->size(2)))
+    return none();
+  const at::Tensor* o_lo = nullptr;
+  if (a[12] != Py_None) {
+    o_lo = gpu_tensor(a[12]);
+    if (!o_lo || !like(*o_lo, *q, dt) || o_lo->sizes() != q->sizes() || !o_lo->is_contiguous()) return none();
+  }
+  int need[3];
+  for (int i = 0; i < 3; ++i)
+    if ((need[i] = PyObject_IsTrue(a[8 + i])) < 0) {
+      PyErr_Clear();
+      return none();
+    }
+  mea_problem p;
+  mea_score s;
+  if (!problem(&p, q->size(0), q->size(1), q->size(2), k->size(2), q->size(3), q->size(3), dtype_code(dt), a[6], a[7], a[11],
+               q->device(), false) ||
+      !score(&s, a + 13, *q, *k, &bias)) {
+    PyErr_Clear();
+    return none();
+  }
+  if (!bias) need[2] = 0;
+  if (!(need[0] || need[1] || need[2])) return none();
+  at::Tensor dq, dk, dv, db;
+  mea_status st;
+  {
+    pybind11::gil_scoped_release no_gil;
+    const auto opts = at::TensorOptions().dtype(dt).device(q->device());
+    size_t bytes = 0;
+    st = g_scored_bwd_ws(&p, &s, &bytes);
+    if (st == MEA_OK) {
+      if (need[0] || need[2]) dq = at::empty(q->sizes(), opts);
+      if (need[1]) {
+        dk = at::empty(k->sizes(), opts);
+        dv = at::empty(k->sizes(), opts);
+      }
+      if (need[2]) db = at::empty(bias->sizes(), opts.dtype(bias->scalar_type()));
+      mea_strides ms = {};
+      if (!q->is_contiguous() || !k->is_contiguous() || !v->is_contiguous() || !o->is_contiguous() || !d_o->is_contiguous()) {
+        ms.q = strides_of(*q);
+        ms.k = strides_of(*k);
+        ms.v = strides_of(*v);
+        ms.o = strides_of(*o);
+        ms.d_o = strides_of(*d_o);
+        if (dq.defined()) ms.dq = strides_of(dq);
+        if (dk.defined()) ms.dk = ms.dv = strides_of(dk);
+        p.strides = &ms;
+      }
+      at::Tensor ws = workspace(bytes, q->device());
+      auto ptr = [](at::Tensor& t) { return t.defined() ? t.mutable_data_ptr() : nullptr; };
+      st = g_scored_bwd(&p, &s, q->const_data_ptr(), k->const_data_ptr(), v->const_data_ptr(), o->const_data_ptr(),
+                        o_lo ? o_lo->const_data_ptr() : nullptr, d_o->const_data_ptr(),
+                        static_cast<const float*>(lse->const_data_ptr()), ptr(dq), ptr(dk), ptr(dv), ptr(db),
+                        ws.mutable_data_ptr(), bytes, stream_of(q->device()));
+    }
+  }
+  if (st != MEA_OK) return failed("mea_scored_attention_bwd", st);
+  if (!need[0]) dq = at::Tensor();
+  return tuple_of({dq, dk, dv, db});
+  END_HANDLE_TH_ERRORS
+}
+
+// prefix_fwd(q, k_prefix, v_prefix, k, v, causal, scale, kv_len, q_pos, out,
+// need_lse): (o, lse), or None.
+PyObject* ext_prefix_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  if (n != 11) return none();
+  const at::Tensor *q = gpu_tensor(a[0]), *kp = gpu_tensor(a[1]), *vp = gpu_tensor(a[2]), *k = gpu_tensor(a[3]),
+                   *v = gpu_tensor(a[4]);
+  if (!q || !kp || !vp || !k || !v) return none();
+  const at::ScalarType dt = q->scalar_type();
+  if (dtype_code(dt) < 0 || !in_place(*q) || !like(*k, *q, dt) || !like(*v, *q, dt) || !grouped_shapes(*q, *k, *v))
+    return none();
+  const int64_t unit = 16 / q->element_size();
+  for (const at::Tensor* t : {kp, vp})
+    if (t->device() != q->device() || t->scalar_type() != dt || t->dim() != 3 || t->stride(2) != 1 ||
+        reinterpret_cast<uintptr_t>(t->const_data_ptr()) % 16 || t->stride(0) % unit || t->stride(1) % unit ||
+        t->size(0) != k->size(1) || t->size(2) != q->size(3) || t->size(1) != kp->size(1))
+      return none();
+  const at::Tensor* out = nullptr;
+  if (a[9] != Py_None) {
+    out = gpu_tensor(a[9]);
+    if (!out || !like(*out, *q, dt) || out->sizes() != q->sizes()) return none();
+  }
+  const int need_lse = PyObject_IsTrue(a[10]);
+  mea_problem p;
+  mea_shared_prefix x = {};
+  const void* pos;
+  if (need_lse < 0 ||
+      !problem(&p, q->size(0), q->size(1), q->size(2), k->size(2), q->size(3), q->size(3), dtype_code(dt), a[5], a[6], a[7],
+               q->device(), false) ||
+      !vector_ok(a[8], q->device(), at::kInt, {q->size(0)}, &pos)) {
+    PyErr_Clear();
+    return none();
+  }
+  x.kv_heads = k->size(1);
+  x.n_p = kp->size(1);
+  x.k = kp->const_data_ptr();
+  x.v = vp->const_data_ptr();
+  x.k_strides = mea_tensor_strides{0, kp->stride(0), kp->stride(1)};
+  x.v_strides = mea_tensor_strides{0, vp->stride(0), vp->stride(1)};
+  x.q_pos = static_cast<const int32_t*>(pos);
+  at::Tensor o, lse;
+  mea_status st;
+  {
+    pybind11::gil_scoped_release no_gil;
+    size_t bytes = 0;
+    st = g_prefix_ws(&p, &x, &bytes);
+    if (st == MEA_OK) {
+      o = out ? *out : at::empty(q->sizes(), at::TensorOptions().dtype(dt).device(q->device()));
+      if (need_lse) lse = at::empty(q->sizes().slice(0, 3), at::TensorOptions().dtype(at::kFloat).device(q->device()));
+      mea_strides ms = {};
+      if (!q->is_contiguous() || !k->is_contiguous() || !v->is_contiguous() || !o.is_contiguous()) {
+        ms.q = strides_of(*q);
+        ms.k = strides_of(*k);
+        ms.v = strides_of(*v);
+        ms.o = strides_of(o);
+        p.strides = &ms;
+      }
+      at::Tensor ws = workspace(bytes, q->device());
+      st = g_prefix_fwd(&p, &x, q->const_data_ptr(), k->const_data_ptr(), v->const_data_ptr(), o.mutable_data_ptr(),
+                        need_lse ? static_cast<float*>(lse.mutable_data_ptr()) : nullptr, ws.mutable_data_ptr(), bytes,
+                        stream_of(q->device()));
+    }
+  }
+  if (st != MEA_OK) return failed("mea_prefix_attention_fwd", st);
+  return tuple_of({o, lse});
+  END_HANDLE_TH_ERRORS
+}
+
+// init_scored(<addresses in the order of _lib.NATIVE_SCORED_CALLS>).
+PyObject* ext_init_scored(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (n != 6) {
+    PyErr_SetString(PyExc_TypeError, "init_scored takes six addresses");
+    return nullptr;
+  }
+  void* f[6];
+  for (int i = 0; i < 6; ++i) {
+    f[i] = PyLong_AsVoidPtr(a[i]);
+    if (PyErr_Occurred()) return nullptr;
+  }
+  g_scored_fwd_ws = reinterpret_cast<decltype(g_scored_fwd_ws)>(f[0]);
+  g_scored_bwd_ws = reinterpret_cast<decltype(g_scored_bwd_ws)>(f[1]);
+  g_scored_fwd = reinterpret_cast<decltype(g_scored_fwd)>(f[2]);
+  g_scored_bwd = reinterpret_cast<decltype(g_scored_bwd)>(f[3]);
+  g_prefix_ws = reinterpret_cast<decltype(g_prefix_ws)>(f[4]);
+  g_prefix_fwd = reinterpret_cast<decltype(g_prefix_fwd)>(f[5]);
+  Py_RETURN_NONE;
+}
+
 // init(check, fwd_workspace_size, bwd_workspace_size, fwd, bwd): _lib.check and
 // the addresses of the library's entry points.
 PyObject* ext_init(PyObject*, PyObject* const* a, Py_ssize_t n) {
@@ -400,6 +690,10 @@ PyMethodDef methods[] = {
     {"bwd", fast(ext_bwd), METH_FASTCALL, nullptr},
     {"packed_fwd", fast(ext_packed_fwd), METH_FASTCALL, nullptr},
     {"packed_bwd", fast(ext_packed_bwd), METH_FASTCALL, nullptr},
+    {"init_scored", fast(ext_init_scored), METH_FASTCALL, nullptr},
+    {"scored_fwd", fast(ext_scored_fwd), METH_FASTCALL, nullptr},
+    {"scored_bwd", fast(ext_scored_bwd), METH_FASTCALL, nullptr},
+    {"prefix_fwd", fast(ext_prefix_fwd), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 

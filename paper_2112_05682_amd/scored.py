@@ -63,6 +63,27 @@ def _side(buckets: int, two_sided: bool, max_distance: int):
     return (ctypes.c_int32 * len(edges))(*edges)
 
 
+@functools.lru_cache(maxsize=None)
+def _side_arg(buckets: int, two_sided: bool, max_distance: int):
+    """The same for the native calls: address, number and whether there are two sides."""
+    edges = _side(buckets, two_sided, max_distance)
+    return ctypes.addressof(edges), len(edges), two_sided
+
+
+def _native_score(causal, softcap, slopes, bias, max_distance, bidirectional, docs, prefix_len, q_pos):
+    """The native calls' last arguments, or None where only the general path can say what
+    is wrong."""
+    if prefix_len is not None and not causal:
+        return None
+    side = None
+    if bias is not None:
+        if not isinstance(bias, torch.Tensor) or bias.dim() != 2:
+            return None
+        side = _side_arg(bias.shape[0], not causal if bidirectional is None else bool(bidirectional), int(max_distance))
+    q_doc, k_doc = docs if isinstance(docs, tuple) and len(docs) == 2 else (docs, docs)
+    return softcap, slopes, bias, side, q_doc, k_doc, prefix_len, q_pos
+
+
 def _int32(name, t, shape, device):
     if t is None:
         return None
@@ -154,6 +175,11 @@ def attention_scored_fwd(q, k, v, causal: bool = False, scale: float | None = No
     none, or a pair of those of the queries and of the keys.  ``prefix_len``, ``q_pos`` (position of
     the first query; 0 without it, negative values read as 0) and ``kv_len``: int32 ``[B]``.  For a
     step of decoding against a cache, ``q_pos = kv_len - n_q``."""
+    mods = _native_score(causal, softcap, slopes, bias, max_distance, bidirectional, docs, prefix_len, q_pos)
+    if mods is not None:
+        r = _lib.native().scored_fwd(q, k, v, causal, scale, need_lse, out, kv_len, residual, *mods)
+        if r is not None:
+            return r
     _shapes(q, k, v)
     _check_tensors(("q", "k", "v"), (q, k, v), q.dtype, q.device)
     s = _score(q, k, causal, softcap, slopes, bias, max_distance, bidirectional, docs, prefix_len, q_pos)
@@ -178,6 +204,11 @@ def attention_scored_bwd(q, k, v, o, lse, do, causal: bool = False, scale: float
                          bidirectional: bool | None = None, docs=None, prefix_len=None, q_pos=None):
     """Returns ``(dq, dk, dv, dbias)`` for the upstream gradient ``do`` of a forward with the
     same arguments; those not needed (and dbias without a bias) are None."""
+    mods = _native_score(causal, softcap, slopes, bias, max_distance, bidirectional, docs, prefix_len, q_pos)
+    if mods is not None:
+        r = _lib.native().scored_bwd(q, k, v, o, lse, do, causal, scale, need_dq, need_dkdv, need_dbias, kv_len, o_lo, *mods)
+        if r is not None:
+            return r
     _shapes(q, k, v)
     _check_tensors(("q", "k", "v", "o", "do"), (q, k, v, o, do), q.dtype, q.device)
     _check_tensors(("lse",), (lse,), torch.float32, q.device)
@@ -254,6 +285,9 @@ def attention_shared_prefix(q, k_prefix, v_prefix, k, v, causal: bool = False, s
     with ``need_lse``.  For serving: no gradient."""
     if torch.is_grad_enabled() and any(t.requires_grad for t in (q, k_prefix, v_prefix, k, v)):
         raise ValueError("attention_shared_prefix has no gradient: call it under torch.no_grad()")
+    r = _lib.native().prefix_fwd(q, k_prefix, v_prefix, k, v, causal, scale, kv_len, q_pos, out, need_lse)
+    if r is not None:
+        return r if need_lse else r[0]
     _shapes(q, k, v)
     if k_prefix.dim() != 3 or k_prefix.shape != v_prefix.shape or k_prefix.shape[0] != k.shape[1] \
             or k_prefix.shape[2] != q.shape[3]:
