@@ -38,7 +38,7 @@ __device__ __forceinline__ void store_table(const ScoredBwdParams& p, int64_t at
 __global__ __launch_bounds__(256) void scored_table_kernel(ScoredBwdParams p) {
   __shared__ double red[256];
   const int nb = p.s.n_edges * (p.s.two_sided ? 2 : 1);
-  const int64_t parts = (int64_t)p.n_b * p.n_qtiles;
+  const int64_t parts = (int64_t)p.n_b * p.n_qtiles * p.dq_parts;
   const int head = blockIdx.x / nb, e = blockIdx.x % nb;
   double x = 0.0;
   for (int64_t i = threadIdx.x; i < parts; i += 256) x += (double)p.table_part[(head * parts + i) * nb + e];

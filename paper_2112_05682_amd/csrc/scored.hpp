@@ -376,6 +376,12 @@ struct ScoredBwdParams {
   float* lse2;
   float* neg_d;
   float* table_part;  // dS sums by bucket of each dQ workgroup, [n_wgs, buckets], or null
+  // Float32 sums of each part, where a pass has several (BwdParts): [part, B, H_kv, n_k, D]
+  // twice, and [part, B, H, n_q, D].
+  float* dk_part;
+  float* dv_part;
+  float* dq_part;
+  int kv_heads_parts, kv_query_parts, dq_parts;
   void* d_table;      // [buckets, H], the table's type
   int64_t n_q, n_k, n_q_pad;
   int n_b, heads_kv, heads_per_kv;
@@ -384,6 +390,40 @@ struct ScoredBwdParams {
   TensorStrides sq, sk, sv, so, sdo, sdq, sdk, sdv;
   ScoreArgs s;
 };
+
+// Into how many parts dK/dV workgroups split their heads and their queries, and dQ
+// workgroups their keys, where the tiles alone would leave places on the chip empty
+// (the parts' float32 sums are added afterwards, in order): as many as fill the
+// chip's places, twice over with the causal mask, whose tiles differ in length.  Heads
+// before queries, as a part of a head reads the same keys again.  Forward + backward
+// in us with 1 / 2 / 4 / 8 / 16 parts of dK/dV (dQ whole), and as the rule has it:
+// bf16 d = 128 causal 2x16 heads on 4, 4096 (256 workgroups) 1380 / 1022 / 865 / 925 /
+// 1042, rule 4: 862; 3x2 on 1, 3761 (90) 644 / 443 / 347 / 303 / 335, rule 11, dQ 5: 248;
+// 3x24 on 3, 897 (72) 468 / 296 / 209 / 175 / 189, rule 14: 179; d = 64 4x12, 1999 (768)
+// 219 / 234 / 275, rule 1, dQ 1: 207; 4x16, 4096 (2048) 887 / 994; float32 d = 64 2x8 on 4,
+// 700 (48) 219 / 168 / 142 / 135 / 142, rule 10, dQ 6: 122; d = 128 2x4 on 2, 1000 (32) 743
+// / 495 / 374 / 317 / 312, rule 16, dQ 8: 204.
+struct BwdParts {
+  int kv_heads, kv_queries, dq;
+};
+inline BwdParts bwd_parts(bool is16, bool causal, int d, int64_t n_q, int64_t n_k, int64_t batch, int64_t heads,
+                          int64_t heads_kv) {
+  const int64_t G = heads / heads_kv, kv_wgs = batch * heads_kv * ((n_k + 127) / 128), q_wgs = batch * heads * ((n_q + 127) / 128);
+  const int64_t kv_places = is16 ? 512 : 256, q_places = is16 || d == 64 ? 512 : 256;
+  BwdParts r = {1, 1, 1};
+  int64_t want = kv_places * (causal ? 2 : 1) / kv_wgs;
+  const int64_t q_tiles = (n_q + 127) / 128, k_tiles = (n_k + 127) / 128;
+  if (want > 1) {
+    r.kv_heads = (int)(want < G ? want : G);
+    int64_t pq = want / r.kv_heads;
+    if (pq > q_tiles) pq = q_tiles;
+    r.kv_queries = pq < 1 ? 1 : (int)pq;
+  }
+  want = q_places * (causal ? 2 : 1) / q_wgs;
+  if (want > k_tiles) want = k_tiles;
+  if (want > 1) r.dq = (int)want;
+  return r;
+}
 
 hipError_t launch_scored_table(const ScoredBwdParams& p, hipStream_t stream);
 hipError_t launch_doc_ranges(const int* ids, int64_t n, int64_t batches, int2* out, hipStream_t stream);

@@ -190,20 +190,27 @@ bool fits_launch(int64_t wgs) { return wgs < ((int64_t)1 << 31) / 256; }
 
 struct BwdWork {
   int64_t n_q_pad, n_qtiles;
-  size_t rows, ranges_q, ranges_k, table, total;
+  mea::BwdParts parts;
+  size_t rows, ranges_q, ranges_k, table, kv_sums, q_sums, total;
 };
 BwdWork plan_scored_bwd(const mea_problem* p, const mea_score* s) {
   BwdWork w = {};
   w.n_q_pad = (p->n_q + mea::kScoredRowPad - 1) / mea::kScoredRowPad * mea::kScoredRowPad;
   w.n_qtiles = (p->n_q + mea::kScoredDqRows - 1) / mea::kScoredDqRows;
+  const int64_t kv = kv_heads_of(p, s->kv_heads);
+  w.parts = mea::bwd_parts(p->dtype != MEA_F32, p->causal != 0, (int)p->d, p->n_q, p->n_k, p->batch, p->heads, kv);
+  const int kv_parts = w.parts.kv_heads * w.parts.kv_queries;
+  if (kv_parts > 1) w.kv_sums = round256((size_t)kv_parts * (size_t)(p->batch * kv) * (size_t)p->n_k * (size_t)p->d * 4);
+  if (w.parts.dq > 1) w.q_sums = round256((size_t)w.parts.dq * (size_t)(p->batch * p->heads) * (size_t)p->n_q * (size_t)p->d * 4);
   w.rows = round256((size_t)p->batch * (size_t)p->heads * (size_t)w.n_q_pad * 4);
   if (s->q_doc) {
     w.ranges_q = range_bytes(p->batch, p->n_q);
     w.ranges_k = range_bytes(p->batch, p->n_k);
   }
   if (s->table)
-    w.table = round256((size_t)p->batch * (size_t)p->heads * (size_t)w.n_qtiles * (size_t)s->n_edges * (s->two_sided ? 2 : 1) * 4);
-  w.total = 2 * w.rows + w.ranges_q + w.ranges_k + w.table + 256;
+    w.table = round256((size_t)p->batch * (size_t)p->heads * (size_t)w.n_qtiles * (size_t)w.parts.dq *
+                       (size_t)s->n_edges * (s->two_sided ? 2 : 1) * 4);
+  w.total = 2 * w.rows + w.ranges_q + w.ranges_k + w.table + 2 * w.kv_sums + w.q_sums + 256;
   return w;
 }
 
@@ -350,7 +357,8 @@ mea_status mea_scored_attention_bwd(const mea_problem* p, const mea_score* s, co
         (dk && (!strides_ok(B, kv, a.sdk, p->n_k, true, e, d) || !strides_ok(B, kv, a.sdv, p->n_k, true, e, d))))
       return MEA_ERR_INVALID_ARG;
   }
-  if (!fits_launch(p->batch * p->heads * (w.n_q_pad / 8)) || !fits_launch(p->batch * kv * ((p->n_k + 127) / 128)))
+  if (!fits_launch(p->batch * p->heads * (w.n_q_pad / 8)) || !fits_launch(p->batch * kv * ((p->n_k + 127) / 128)) ||
+      !fits_launch((p->batch * (p->heads * p->n_q + 2 * kv * p->n_k) + 24) * p->d / 4 / 256))
     return MEA_ERR_INVALID_ARG;
   if (p->causal)
     a.tile_order = mea::causal_tile_order(p->batch * kv * p->n_k * 2 * p->d * (int64_t)elem_size(p->dtype), 0, false);
@@ -369,6 +377,15 @@ mea_status mea_scored_attention_bwd(const mea_problem* p, const mea_score* s, co
     if (e != hipSuccess) return MEA_ERR_HIP;
   }
   if (d_table) a.table_part = at;
+  at += w.table / 4;
+  a.kv_heads_parts = w.parts.kv_heads;
+  a.kv_query_parts = w.parts.kv_queries;
+  a.dq_parts = w.parts.dq;
+  if (w.kv_sums && dk) {
+    a.dk_part = at;
+    a.dv_part = at + w.kv_sums / 4;
+  }
+  if (w.q_sums && dq) a.dq_part = at + 2 * w.kv_sums / 4;
   const int d = (int)p->d;
   switch (p->dtype) {
     case MEA_F32: return status_of(mea::launch_scored_bwd<float>(a, d, stream));

@@ -97,7 +97,11 @@ __global__ __launch_bounds__(256, (ScoredKvTile<T, D>::OCC)) void scored_dkdv_ke
   const int h = lane >> 5, c = lane & 31;
 
   const TileItem item = tile_item(blockIdx.x, gridDim.x, p.n_ktiles, sa.causal ? p.tile_order : 0);
-  const int b = item.group % p.n_b, kvh = item.group / p.n_b;
+  const int b = item.group % p.n_b, kvh = item.group / p.n_b % p.heads_kv;
+  // This part's heads and its share of the tiles of queries.
+  const int part = item.group / (p.n_b * p.heads_kv);
+  const int part_h = part % p.kv_heads_parts, part_q = part / p.kv_heads_parts;
+  const int g0 = p.heads_per_kv * part_h / p.kv_heads_parts, g_end = p.heads_per_kv * (part_h + 1) / p.kv_heads_parts;
   const int64_t k0 = (int64_t)item.tile * C::BKG, kw = k0 + 32 * wave, key = kw + c;
 
   const int64_t n_kv = batch_keys(sa, b, p.n_k), pos0 = first_pos(sa, b);
@@ -149,14 +153,16 @@ __global__ __launch_bounds__(256, (ScoredKvTile<T, D>::OCC)) void scored_dkdv_ke
   const int n_units = (int)((p.n_q + 31) / 32);
   const int2* const ranges = sa.q_range ? sa.q_range + (int64_t)b * n_units : nullptr;
   DocTiles<QS> docs(ranges, n_units, ids.x, ids.y);
-  const int t_end = k0 < n_kv ? (int)((p.n_q + BQ - 1) / BQ) : 0;
-  int g = 0, t = 0;  // current head and tile
+  const int t_all = k0 < n_kv ? (int)((p.n_q + BQ - 1) / BQ) : 0;
+  const int64_t t_see = q_begin / BQ < t_all ? q_begin / BQ : t_all;
+  const int t_begin = (int)(t_see + (t_all - t_see) * part_q / p.kv_query_parts);
+  const int t_end = (int)(t_see + (t_all - t_see) * (part_q + 1) / p.kv_query_parts);
+  int g = g0, t = 0;  // current head and tile
   auto first_tile = [&]() {
     docs.base = -64;
-    const int64_t f = q_begin / BQ;
-    return docs.next(f < t_end ? (int)f : t_end, t_end);
+    return docs.next(t_begin, t_end);
   };
-  // The tile after (g_, t_); g_ = heads_per_kv at the end.
+  // The tile after (g_, t_); g_ = g_end at the end.
   auto advance = [&](int& g_, int& t_) {
     t_ = docs.next(t_ + 1, t_end);
     if (t_ >= t_end) {
@@ -165,7 +171,7 @@ __global__ __launch_bounds__(256, (ScoredKvTile<T, D>::OCC)) void scored_dkdv_ke
     }
   };
   t = first_tile();
-  if (t >= t_end) g = p.heads_per_kv;  // no query sees these keys
+  if (t >= t_end) g = g_end;  // no query sees these keys
 
   constexpr int CPR = C::CPR;
   const TileCopy<std::conditional_t<F32, __bf16, T>, D, BQ, false> copies(wave, lane, p.sq.r, p.sdo.r);
@@ -356,7 +362,7 @@ __global__ __launch_bounds__(256, (ScoredKvTile<T, D>::OCC)) void scored_dkdv_ke
   };
 
   int buf = 0, g_bias = -1;
-  if (g < p.heads_per_kv) {
+  if (g < g_end) {
     load_rows(g, t);
     if constexpr (F32) {
       load_stage(g, t);
@@ -367,7 +373,7 @@ __global__ __launch_bounds__(256, (ScoredKvTile<T, D>::OCC)) void scored_dkdv_ke
     store_rows(0);
   }
   if constexpr (F32) __syncthreads();
-  while (g < p.heads_per_kv) {
+  while (g < g_end) {
     const bool masked = (int64_t)t * BQ < q_full;
     bool by_doc = false, absent = false;
     if (sa.q_doc) {
@@ -377,7 +383,7 @@ __global__ __launch_bounds__(256, (ScoredKvTile<T, D>::OCC)) void scored_dkdv_ke
     }
     int gn = g, tn = t;
     advance(gn, tn);
-    const bool more = gn < p.heads_per_kv;
+    const bool more = gn < g_end;
     if constexpr (!F32) {
       wait_global_loads();
       __syncthreads();
@@ -422,6 +428,23 @@ __global__ __launch_bounds__(256, (ScoredKvTile<T, D>::OCC)) void scored_dkdv_ke
   }
 
   if (key >= p.n_k) return;
+  if (p.dk_part) {
+    const int64_t at = ((((int64_t)part * p.n_b + b) * p.heads_kv + kvh) * p.n_k + key) * D;
+#pragma unroll
+    for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+      for (int a4 = 0; a4 < 4; ++a4) {
+        f32x4 x, y;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          x[e] = live ? dk[dt][4 * a4 + e] : 0.0f;
+          y[e] = live ? dv[dt][4 * a4 + e] : 0.0f;
+        }
+        *reinterpret_cast<f32x4*>(p.dk_part + at + 32 * dt + 8 * a4 + 4 * h) = x;
+        *reinterpret_cast<f32x4*>(p.dv_part + at + 32 * dt + 8 * a4 + 4 * h) = y;
+      }
+    return;
+  }
   T* dkg = static_cast<T*>(p.dk) + (int64_t)b * p.sdk.b + (int64_t)kvh * p.sdk.h + key * p.sdk.r;
   T* dvg = static_cast<T*>(p.dv) + (int64_t)b * p.sdv.b + (int64_t)kvh * p.sdv.h + key * p.sdv.r;
 #pragma unroll
@@ -479,7 +502,8 @@ __global__ __launch_bounds__(256, (ScoredDqTile<T, D>::OCC)) void scored_dq_kern
   const int qtile = sa.causal ? p.n_qtiles - 1 - item.tile : item.tile;
   // Heads that share a key head are neighbours, then batches.
   const int gi = item.group / p.heads_per_kv;
-  const int b = gi % p.n_b, kvh = gi / p.n_b, head = kvh * p.heads_per_kv + item.group % p.heads_per_kv;
+  const int b = gi % p.n_b, kvh = gi / p.n_b % p.heads_kv, part = gi / (p.n_b * p.heads_kv);
+  const int head = kvh * p.heads_per_kv + item.group % p.heads_per_kv;
   const int64_t q0 = (int64_t)qtile * C::ROWS, qw = q0 + 32 * wave, qi = qw + c;
   const int64_t q_last = (q0 + C::ROWS < p.n_q ? q0 + C::ROWS : p.n_q) - 1;
 
@@ -721,8 +745,9 @@ __global__ __launch_bounds__(256, (ScoredDqTile<T, D>::OCC)) void scored_dq_kern
     }
   };
 
-  const int t_end = (int)((lim_hi + BK - 1) / BK);
-  int t = docs.next(0, t_end), buf = 0;
+  const int64_t t_all = (lim_hi + BK - 1) / BK;
+  const int t_end = (int)(t_all * (part + 1) / p.dq_parts);
+  int t = docs.next((int)(t_all * part / p.dq_parts), t_end), buf = 0;
   if (t < t_end) {
     if constexpr (F32) {
       load_stage(t);
@@ -766,7 +791,18 @@ __global__ __launch_bounds__(256, (ScoredDqTile<T, D>::OCC)) void scored_dq_kern
     t = tn;
   }
 
-  if (in_rows) {
+  if (in_rows && p.dq_part) {
+    float* to = p.dq_part + ((((int64_t)part * p.n_b + b) * sa.heads + head) * p.n_q + qi) * D;
+#pragma unroll
+    for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+      for (int a4 = 0; a4 < 4; ++a4) {
+        f32x4 x;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = live ? acc[dt][4 * a4 + e] : 0.0f;
+        *reinterpret_cast<f32x4*>(to + 32 * dt + 8 * a4 + 4 * h) = x;
+      }
+  } else if (in_rows) {
     T* dqg = static_cast<T*>(p.dq) + (int64_t)b * p.sdq.b + (int64_t)head * p.sdq.h + qi * p.sdq.r;
 #pragma unroll
     for (int dt = 0; dt < NDT; ++dt)
@@ -804,8 +840,8 @@ __global__ __launch_bounds__(256, (ScoredDqTile<T, D>::OCC)) void scored_dq_kern
     }
     __syncthreads();
     const int nb = sa.n_edges * (sa.two_sided ? 2 : 1), zero = sa.span + kPad;  // place of distance 0
-    // Workgroups of one head are neighbours in table_part: [head][batch][query tile].
-    float* part = p.table_part + (((int64_t)head * p.n_b + b) * p.n_qtiles + qtile) * nb;
+    // Workgroups of one head are neighbours in table_part: [head][batch][query tile][part].
+    float* const to = p.table_part + ((((int64_t)head * p.n_b + b) * p.n_qtiles + qtile) * p.dq_parts + part) * nb;
     for (int e = tid; e < nb; e += C::NT) {
       const bool ahead = e >= sa.n_edges;
       const int s = ahead ? e - sa.n_edges : e;
@@ -821,12 +857,49 @@ __global__ __launch_bounds__(256, (ScoredDqTile<T, D>::OCC)) void scored_dq_kern
       }
       float y = 0.0f;
       for (int x = lo; x < end; ++x) y += bins[x];
-      part[e] = y;
+      to[e] = y;
     }
   }
 }
 
+// The parts' sums, added in order, scaled and rounded: blocks of rows of dK, of dV, of
+// dQ; a thread per row and 4 features.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void scored_bwd_sum_kernel(ScoredBwdParams p, int64_t kv_blocks) {
+  constexpr int G4 = D / 4;
+  int64_t block = blockIdx.x;
+  const int which = p.dk_part ? (block < kv_blocks ? 0 : (block < 2 * kv_blocks ? 1 : 2)) : 2;
+  if (p.dk_part) block -= which * kv_blocks;
+  const int heads = which == 2 ? p.s.heads : p.heads_kv, parts = which == 2 ? p.dq_parts : p.kv_heads_parts * p.kv_query_parts;
+  const int64_t n = which == 2 ? p.n_q : p.n_k, rows = (int64_t)p.n_b * heads * n;
+  const int64_t gid = block * 256 + threadIdx.x, row = gid / G4;
+  const int f0 = 4 * (int)(gid % G4);
+  if (row >= rows) return;
+  const float* from = (which == 0 ? p.dk_part : which == 1 ? p.dv_part : p.dq_part) + row * D + f0;
+  f32x4 x = *reinterpret_cast<const f32x4*>(from);
+  for (int i = 1; i < parts; ++i) x += *reinterpret_cast<const f32x4*>(from + (int64_t)i * rows * D);
+  const TensorStrides st = which == 0 ? p.sdk : which == 1 ? p.sdv : p.sdq;
+  T* to = static_cast<T*>(which == 0 ? p.dk : which == 1 ? p.dv : p.dq) + row / n / heads * st.b + row / n % heads * st.h +
+          row % n * st.r + f0;
+  const float f = which == 1 ? 1.0f : p.scale;
+  typename FragT<T>::half y;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) y[e] = (T)(x[e] * f);
+  *reinterpret_cast<typename FragT<T>::half*>(to) = y;
+}
+
 // ------------------------------------------------------------------ launchers
+template <typename T, int D>
+static hipError_t launch_scored_sum(const ScoredBwdParams& p, hipStream_t stream) {
+  ScoredBwdParams a = p;
+  auto blocks = [](int64_t rows) { return (rows * (D / 4) + 255) / 256; };
+  int64_t kv = blocks((int64_t)p.n_b * p.heads_kv * p.n_k);
+  const int64_t grid = (p.dk_part ? 2 * kv : 0) + (p.dq_part ? blocks((int64_t)p.n_b * p.s.heads * p.n_q) : 0);
+  if (!grid) return hipSuccess;
+  void* args[] = {&a, &kv};
+  return hipLaunchKernel(reinterpret_cast<const void*>(scored_bwd_sum_kernel<T, D>), dim3((unsigned)grid), dim3(256), args, 0,
+                         stream);
+}
 template <typename T, int D, bool CAP, bool BIAS>
 static hipError_t launch_scored_bwd_kernels(const ScoredBwdParams& p, hipStream_t stream) {
   using K = ScoredKvTile<T, D>;
@@ -839,17 +912,17 @@ static hipError_t launch_scored_bwd_kernels(const ScoredBwdParams& p, hipStream_
   hipError_t e = hipSuccess;
   if (p.dk) {
     e = hipLaunchKernel(reinterpret_cast<const void*>(scored_dkdv_kernel<T, D, CAP, BIAS>),
-                        dim3((unsigned)((int64_t)a.n_ktiles * p.n_b * p.heads_kv)), dim3(K::NT), args, K::LDS_BYTES + bias,
+                        dim3((unsigned)((int64_t)a.n_ktiles * p.n_b * p.heads_kv * p.kv_heads_parts * p.kv_query_parts)), dim3(K::NT), args, K::LDS_BYTES + bias,
                         stream);
     if (e != hipSuccess) return e;
   }
-  if (!p.dq) return e;
+  if (!p.dq) return launch_scored_sum<T, D>(a, stream);
   const int bins = p.table_part ? (4 * bias_places(p.s) + 8192) * 4 : 0;
   e = hipLaunchKernel(reinterpret_cast<const void*>(scored_dq_kernel<T, D, CAP, BIAS>),
-                      dim3((unsigned)((int64_t)a.n_qtiles * p.n_b * p.s.heads)), dim3(Q::NT), args,
+                      dim3((unsigned)((int64_t)a.n_qtiles * p.n_b * p.s.heads * p.dq_parts)), dim3(Q::NT), args,
                       Q::LDS_BYTES + bias + bins, stream);
-  if (e != hipSuccess || !p.table_part) return e;
-  return launch_scored_table(a, stream);
+  if (e == hipSuccess && p.table_part) e = launch_scored_table(a, stream);
+  return e != hipSuccess ? e : launch_scored_sum<T, D>(a, stream);
 }
 template <typename T, int D>
 static hipError_t launch_scored_bwd_d(const ScoredBwdParams& p, hipStream_t stream) {
