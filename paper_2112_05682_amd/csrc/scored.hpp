@@ -431,6 +431,9 @@ hipError_t launch_doc_ranges(const int* ids, int64_t n, int64_t batches, int2* o
 // Rows per workgroup: 32 for each of 4 waves, or 2 or 1 (the other waves take
 // shares of the keys).
 template <typename T> hipError_t launch_stream(const StreamParams& p, int d, int row_waves, hipStream_t stream);
+// Two key sets in one launch: row waves 4 and 4 or 2, or 1 and 1 (float32: 2 and 2).
+template <typename T>
+hipError_t launch_stream_pair(const StreamParams& a, const StreamParams& b, int d, int rwa, int rwb, hipStream_t stream);
 template <typename T>
 hipError_t launch_scored_combine(const StreamParams& p, int d, int n_parts, hipStream_t stream);
 template <typename T> hipError_t launch_scored_bwd(const ScoredBwdParams& p, int d, hipStream_t stream);

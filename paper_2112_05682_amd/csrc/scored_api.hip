@@ -90,37 +90,44 @@ struct StreamPlan {
   int64_t fold, groups, rows, rtiles, splits;  // rows of a group
 };
 
+// Workgroups of these row waves that the chip holds at once.
+int64_t places_of(const mea_problem* p, int row_waves) {
+  if (p->dtype == MEA_F32) return 256;
+  return 256 * (row_waves == 1 && p->d == 128 ? 1 : 2);
+}
+// Row tiles, and key ranges for the places that `taken` workgroups leave.
+void set_tiles(StreamPlan* pl, const mea_problem* p, int rw, int64_t n_keys, int64_t taken) {
+  pl->row_waves = rw;
+  pl->rtiles = (pl->rows + 32 * rw - 1) / (32 * rw);
+  const int64_t wgs = pl->groups * pl->rtiles, tile = mea::stream_tile(p->dtype != MEA_F32, rw);
+  const int64_t key_tiles = (n_keys + tile - 1) / tile, places = places_of(p, rw);
+  int64_t splits = (places - (taken < places / 2 ? taken : places / 2)) / wgs;
+  if (splits > key_tiles / 2) splits = key_tiles / 2;
+  if (splits > 64) splits = 64;
+  pl->splits = splits < 1 ? 1 : splits;
+}
+
 // Fold: with few queries the heads that share a key head are rows of the same
 // tile, so that the keys are read once for all of them; with many, each head has
 // tiles of its own (the keys are then found in L2).  Row waves: as few as hold
 // the rows, and on small grids fewer still, so that the waves without rows of
 // their own take shares of the keys instead.  Splits: enough key ranges for about
 // one workgroup for each place on the chip, of at least two tiles each.
-StreamPlan plan_stream(const mea_problem* p, const ScoreArgs& s, int64_t kv_heads, bool shared, int64_t n_keys) {
+StreamPlan plan_stream(const mea_problem* p, const ScoreArgs& s, int64_t kv_heads) {
   StreamPlan pl;
   const bool is16 = p->dtype != MEA_F32;
   const int64_t G = p->heads / kv_heads;
-  const int least = is16 ? 1 : 2;
-  pl.fold = shared || G * p->n_q <= 64 ? G : 1;
+  pl.fold = G * p->n_q <= 64 ? G : 1;
   // The biases of the folded heads have to fit beside the stages.
   if (pl.fold > 1 && mea::bias_lds_bytes(s, (int)pl.fold) > 24 * 1024) pl.fold = 1;
-  pl.rows = (shared ? p->batch : 1) * p->n_q * pl.fold;
-  pl.groups = (p->heads / pl.fold) * (shared ? 1 : p->batch);
+  pl.rows = p->n_q * pl.fold;
+  pl.groups = p->heads / pl.fold * p->batch;
   const int64_t tiles128 = pl.groups * ((pl.rows + 127) / 128);
   int rw = tiles128 <= 128 ? 1 : (tiles128 <= 256 ? 2 : 4);
   if (pl.rows <= 32) rw = 1;
   else if (pl.rows <= 64 && rw > 2) rw = 2;
   if (!is16) rw = pl.rows <= 64 || tiles128 <= 32 ? 2 : 4;
-  if (rw < least) rw = least;
-  pl.row_waves = rw;
-  pl.rtiles = (pl.rows + 32 * rw - 1) / (32 * rw);
-  const int64_t wgs = pl.groups * pl.rtiles;
-  const int64_t key_tiles = (n_keys + mea::stream_tile(is16, rw) - 1) / mea::stream_tile(is16, rw);
-  int64_t places = 256 * (is16 ? (rw == 1 ? (p->d == 64 ? 2 : 1) : 2) : 1);
-  int64_t splits = wgs * 2 > places ? 1 : places / wgs;
-  if (splits > key_tiles / 2) splits = key_tiles / 2;
-  if (splits > 64) splits = 64;
-  pl.splits = splits < 1 ? 1 : splits;
+  set_tiles(&pl, p, rw, p->n_k, 0);
   return pl;
 }
 
@@ -141,7 +148,7 @@ struct FwdWork {
 };
 FwdWork plan_scored_fwd(const mea_problem* p, const mea_score* s) {
   FwdWork w;
-  w.pl = plan_stream(p, score_args(p, s), kv_heads_of(p, s->kv_heads), false, p->n_k);
+  w.pl = plan_stream(p, score_args(p, s), kv_heads_of(p, s->kv_heads));
   w.ranges = s->q_doc ? range_bytes(p->batch, p->n_k) : 0;
   w.total = w.ranges + (w.pl.splits > 1 ? part_bytes(p, w.pl.splits) : 0);
   if (w.total) w.total += 256;
@@ -229,10 +236,26 @@ struct PrefixWork {
 };
 PrefixWork plan_prefix(const mea_problem* p, const mea_shared_prefix* x) {
   PrefixWork w;
-  const ScoreArgs none = score_args(p, nullptr);
-  const int64_t kv = kv_heads_of(p, x->kv_heads);
-  w.shared = plan_stream(p, none, kv, true, x->n_p);
-  w.own = plan_stream(p, none, kv, false, p->n_k);
+  const bool is16 = p->dtype != MEA_F32;
+  const int64_t kv = kv_heads_of(p, x->kv_heads), G = p->heads / kv;
+  // Both key sets fold the heads of a key head; the prefix also all sequences.
+  w.shared.fold = w.own.fold = G;
+  w.shared.groups = kv;
+  w.shared.rows = p->batch * p->n_q * G;
+  w.own.groups = kv * p->batch;
+  w.own.rows = p->n_q * G;
+  // Four row waves read the prefix a quarter as often as one does, which pays on large
+  // ones; short or few rows rather share the keys of a tile.  us, row waves 1 / 4, at the
+  // best number of ranges each, bf16 d = 128: 256 rows of 8 key heads on 16384 keys 73 / 64,
+  // 800 of 8 on 30000 281 / 164, 864 of 3 on 1329 30 / 32, 64 of 8 on 8192 30 / 31; d = 64: 512
+  // of 4 on 4000 24 / 27.
+  const bool large = w.shared.rows > 64 && (double)(kv * w.shared.rows) * (double)x->n_p > 16e6;
+  const int own_least = w.own.rows <= 64 ? 2 : 4;
+  const int rwa = large || w.own.rows > 64 ? 4 : (is16 && w.own.rows <= 32 ? 1 : (is16 ? 4 : 2));
+  const int rwb = rwa == 4 ? own_least : rwa;
+  set_tiles(&w.own, p, rwb, p->n_k, 0);
+  if (w.own.splits > 8) w.own.splits = 8;
+  set_tiles(&w.shared, p, rwa, x->n_p, w.own.groups * w.own.rtiles * w.own.splits);
   w.total = part_bytes(p, w.shared.splits + w.own.splits) + 256;
   return w;
 }
@@ -435,7 +458,7 @@ mea_status mea_prefix_attention_fwd(const mea_problem* p, const mea_shared_prefi
       !strides_ok(p->batch, kv, own.sv, p->n_k, false, e, d) || !strides_ok(p->batch, p->heads, own.so, p->n_q, true, e, d) ||
       !strides_ok(1, kv, spk, x->n_p, false, e, d) || !strides_ok(1, kv, spv, x->n_p, false, e, d))
     return MEA_ERR_INVALID_ARG;
-  if (!fits_launch(w.own.rtiles * w.own.groups * w.own.splits) || !fits_launch(w.shared.rtiles * w.shared.groups * w.shared.splits) ||
+  if (!fits_launch(w.own.rtiles * w.own.groups * w.own.splits + w.shared.rtiles * w.shared.groups * w.shared.splits) ||
       !fits_launch((own.out_rows * d / 4 + 255) / 256))
     return MEA_ERR_INVALID_ARG;
   const int64_t parts = w.shared.splits + w.own.splits;
@@ -456,8 +479,13 @@ mea_status mea_prefix_attention_fwd(const mea_problem* p, const mea_shared_prefi
   pre.part_o = own.part_o;
   pre.part_m = own.part_m;
   pre.part_l = own.part_l;
-  hipError_t err = run_stream(pre, p, w.shared.row_waves, stream);
-  if (err == hipSuccess) err = run_stream(own, p, w.own.row_waves, stream);
+  const int dd = (int)d, ra = w.shared.row_waves, rb = w.own.row_waves;
+  hipError_t err;
+  switch (p->dtype) {
+    case MEA_F32: err = mea::launch_stream_pair<float>(pre, own, dd, ra, rb, stream); break;
+    case MEA_F16: err = mea::launch_stream_pair<_Float16>(pre, own, dd, ra, rb, stream); break;
+    default: err = mea::launch_stream_pair<__bf16>(pre, own, dd, ra, rb, stream);
+  }
   if (err == hipSuccess) err = run_combine(own, p, (int)parts, stream);
   return status_of(err);
 }

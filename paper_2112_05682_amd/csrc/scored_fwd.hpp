@@ -38,8 +38,9 @@ struct StreamTile {
   static_assert((LDS_BYTES + kBiasMax) * OCC <= 160 * 1024, "LDS");
 };
 
+// Workgroup `block` of n_blocks.
 template <typename T, int D, int RW, bool CAP, bool BIAS>
-__global__ __launch_bounds__(256, (StreamTile<T, D, RW>::OCC)) void scored_stream_kernel(StreamParams p) {
+__device__ __forceinline__ void stream_workgroup(const StreamParams& p, int block, int n_blocks) {
   using C = StreamTile<T, D, RW>;
   using LE = typename Planes<T>::E;
   constexpr bool F32 = C::F32;
@@ -55,7 +56,7 @@ __global__ __launch_bounds__(256, (StreamTile<T, D, RW>::OCC)) void scored_strea
   const int wave_q = RW == 4 ? wave : wave % RW, wave_k = RW == 4 ? 0 : wave / RW;
 
   // ---- workgroup -> row tile, group, key range.
-  const TileItem item = tile_item(blockIdx.x, gridDim.x, p.n_rtiles, p.tile_order);
+  const TileItem item = tile_item(block, n_blocks, p.n_rtiles, p.tile_order);
   const int rtile = sa.causal ? p.n_rtiles - 1 - item.tile : item.tile;  // longest rows first
   const int split = item.group / p.n_groups;
   int gi = item.group % p.n_groups;
@@ -64,32 +65,39 @@ __global__ __launch_bounds__(256, (StreamTile<T, D, RW>::OCC)) void scored_strea
   const int b0 = gi % p.n_b, kvh = gi / p.n_b;
   const int head0 = kvh * p.heads_per_kv + sub * p.fold;
 
-  // ---- this lane's row.
-  const int64_t row0 = (int64_t)rtile * C::ROWS;
-  const int64_t row_last = (row0 + C::ROWS < p.group_rows ? row0 + C::ROWS : p.group_rows) - 1;
-  const int64_t row = row0 + 32 * wave_q + c;
-  const bool in_rows = row < p.group_rows;
-  const int64_t rr = in_rows ? row : row_last;
-  const int g = (int)(rr % p.fold);
-  const int64_t x = rr / p.fold;
-  const int64_t qi = x % p.n_q;
-  const int b = b0 + (int)(x / p.n_q);
-  const int head = head0 + g;
+  // ---- this lane's row.  Rows of a group, keys and positions are below 2^31.
+  const uint32_t n_rows = (uint32_t)p.group_rows, fold = (uint32_t)p.fold;
+  const uint32_t row0 = (uint32_t)rtile * C::ROWS;
+  const uint32_t row_last = (row0 + C::ROWS < n_rows ? row0 + C::ROWS : n_rows) - 1;
+  const uint32_t row = row0 + 32 * wave_q + c;
+  const bool in_rows = row < n_rows;
+  const uint32_t rr = in_rows ? row : row_last;
+  uint32_t g = 0, qu = rr;
+  int b = b0;
+  if (fold > 1) {
+    qu = rr / fold;
+    g = rr - qu * fold;
+  }
+  if (p.batches > 1) {
+    const uint32_t x = qu / (uint32_t)p.n_q;
+    qu -= x * (uint32_t)p.n_q;
+    b = (int)x;
+  }
+  const int64_t qi = qu;
+  const int head = head0 + (int)g;
 
   const int64_t n_kv = batch_keys(sa, b0, p.n_k);
   const int64_t pos0 = first_pos(sa, b0), reach = key_reach(sa, b0, p.n_k);
-  // Keys and positions are below 2^31, so that per-lane ones are 32 bits.
   const int pos = (int)(pos0 + qi);
   int lim = in_rows ? (int)key_limit(n_kv, reach, pos0 + qi) : 0;
   // Limits grow with the query, so the tile's first and last rows bound them (a
-  // group of several batches has no positional mask).
-  const int64_t lim_hi = key_limit(n_kv, reach, pos0 + (row_last / p.fold) % p.n_q);
-  const int64_t lim_lo = key_limit(n_kv, reach, pos0 + (row0 / p.fold) % p.n_q);
-  const int64_t w_row0 = row0 + 32 * wave_q;
-  const int64_t w_last = w_row0 + 31 < p.group_rows ? w_row0 + 31 : p.group_rows - 1;
-  // The wave's first and last query (uniform), and its limit.
-  const bool wave_rows = w_row0 < p.group_rows;
-  const int64_t wq_lo = pos0 + w_row0 / p.fold % p.n_q, wq_hi = pos0 + (wave_rows ? w_last / p.fold % p.n_q : 0);
+  // group of several batches has no positional mask: every limit is n_kv).
+  auto pos_of = [&](uint32_t r) { return pos0 + (fold > 1 ? r / fold : r); };
+  const int64_t lim_hi = key_limit(n_kv, reach, pos_of(row_last)), lim_lo = key_limit(n_kv, reach, pos_of(row0));
+  const uint32_t w_row0 = row0 + 32 * wave_q;
+  const bool wave_rows = w_row0 < n_rows;
+  // The wave's first and last position (uniform), and its limit.
+  const int64_t wq_lo = pos_of(w_row0), wq_hi = pos_of(w_row0 + 31 < n_rows ? w_row0 + 31 : n_rows - 1);
   const int64_t w_lim = wave_rows ? key_limit(n_kv, reach, wq_hi) : 0;
 
   int doc = -2;
@@ -244,14 +252,14 @@ __global__ __launch_bounds__(256, (StreamTile<T, D, RW>::OCC)) void scored_strea
       if (sa.table) {
         const int hi = bias_ahead(sa), last = bias_places(sa) - 1;
         if (k0 + BKW - 1 <= wq_lo - sa.span || k0 >= wq_hi + hi) {  // one value for every key of a row
-          add += bias_at(sa, lds_bias, p.fold, g, k0 >= wq_hi + hi ? last : 0);
+          add += bias_at(sa, lds_bias, p.fold, (int)g, k0 >= wq_hi + hi ? last : 0);
         } else {
           asm volatile("");
 #pragma unroll
           for (int kt = 0; kt < NKT; ++kt) {
             const int64_t ka = k0 + 32 * kt;
             if (ka + 31 <= wq_lo - sa.span || ka >= wq_hi + hi) {
-              const float v = bias_at(sa, lds_bias, p.fold, g, ka >= wq_hi + hi ? last : 0);
+              const float v = bias_at(sa, lds_bias, p.fold, (int)g, ka >= wq_hi + hi ? last : 0);
 #pragma unroll
               for (int r = 0; r < 16; ++r) s[kt][r] += v;
             } else if (p.fold == 1) {
@@ -261,7 +269,7 @@ __global__ __launch_bounds__(256, (StreamTile<T, D, RW>::OCC)) void scored_strea
             } else {
 #pragma unroll
               for (int r = 0; r < 16; ++r)
-                s[kt][r] += bias_at(sa, lds_bias, p.fold, g, off + 32 * kt + permuted_row(r, 0) + sa.span + kPad);
+                s[kt][r] += bias_at(sa, lds_bias, p.fold, (int)g, off + 32 * kt + permuted_row(r, 0) + sa.span + kPad);
             }
           }
         }
@@ -465,6 +473,19 @@ __global__ __launch_bounds__(256, (StreamTile<T, D, RW>::OCC)) void scored_strea
   }
 }
 
+template <typename T, int D, int RW, bool CAP, bool BIAS>
+__global__ __launch_bounds__(256, (StreamTile<T, D, RW>::OCC)) void scored_stream_kernel(StreamParams p) {
+  stream_workgroup<T, D, RW, CAP, BIAS>(p, (int)blockIdx.x, (int)gridDim.x);
+}
+
+// A shared prefix (the first n_a workgroups) and the own keys in one launch, so that
+// the one fills what the other leaves of the chip.
+template <typename T, int D, int RWA, int RWB>
+__global__ __launch_bounds__(256, (StreamTile<T, D, RWA>::OCC)) void scored_pair_kernel(StreamParams a, StreamParams b, int n_a) {
+  if ((int)blockIdx.x < n_a) stream_workgroup<T, D, RWA, false, false>(a, (int)blockIdx.x, n_a);
+  else stream_workgroup<T, D, RWB, false, false>(b, (int)blockIdx.x - n_a, (int)gridDim.x - n_a);
+}
+
 // Combine of the summaries of n_parts key ranges (Section 4): rescaled to the
 // common maximum, added, divided.  A thread per row and 4 features.
 template <typename T, int D>
@@ -517,6 +538,37 @@ __global__ __launch_bounds__(256) void scored_combine_kernel(StreamParams p, int
 }
 
 // ------------------------------------------------------------------ launchers
+template <typename T, int D, int RWA, int RWB>
+static hipError_t launch_pair_kernel(const StreamParams& a, const StreamParams& b, hipStream_t stream) {
+  using A = StreamTile<T, D, RWA>;
+  using B = StreamTile<T, D, RWB>;
+  StreamParams x = a, y = b;
+  x.n_rtiles = (int)((a.group_rows + A::ROWS - 1) / A::ROWS);
+  y.n_rtiles = (int)((b.group_rows + B::ROWS - 1) / B::ROWS);
+  constexpr int lds = A::LDS_BYTES > B::LDS_BYTES ? A::LDS_BYTES : B::LDS_BYTES;
+  const int64_t n_a = (int64_t)x.n_rtiles * a.n_groups * a.n_splits, n_b = (int64_t)y.n_rtiles * b.n_groups * b.n_splits;
+  if (n_a < 1 || n_b < 1 || n_a + n_b >= ((int64_t)1 << 31)) return hipErrorInvalidValue;
+  int na = (int)n_a;
+  void* args[] = {&x, &y, &na};
+  return hipLaunchKernel(reinterpret_cast<const void*>(scored_pair_kernel<T, D, RWA, RWB>), dim3((unsigned)(n_a + n_b)),
+                         dim3(256), args, lds, stream);
+}
+template <typename T, int D>
+static hipError_t launch_pair_rows(const StreamParams& a, const StreamParams& b, int rwa, int rwb, hipStream_t stream) {
+  if (rwa == 4 && rwb == 4) return launch_pair_kernel<T, D, 4, 4>(a, b, stream);
+  if (rwa == 4 && rwb == 2) return launch_pair_kernel<T, D, 4, 2>(a, b, stream);
+  if constexpr (sizeof(T) == 2) {
+    if (rwa == 1 && rwb == 1) return launch_pair_kernel<T, D, 1, 1>(a, b, stream);
+  } else {
+    if (rwa == 2 && rwb == 2) return launch_pair_kernel<T, D, 2, 2>(a, b, stream);
+  }
+  return hipErrorInvalidValue;
+}
+template <typename T>
+hipError_t launch_stream_pair(const StreamParams& a, const StreamParams& b, int d, int rwa, int rwb, hipStream_t stream) {
+  return d == 64 ? launch_pair_rows<T, 64>(a, b, rwa, rwb, stream) : launch_pair_rows<T, 128>(a, b, rwa, rwb, stream);
+}
+
 template <typename T, int D, int RW, bool CAP, bool BIAS>
 static hipError_t launch_stream_kernel(const StreamParams& p, hipStream_t stream) {
   using C = StreamTile<T, D, RW>;
