@@ -126,29 +126,6 @@ __global__ __launch_bounds__(256, (ScoredKvTile<T, D>::OCC)) void scored_dkdv_ke
   const T* __restrict__ kg = static_cast<const T*>(p.k) + (int64_t)b * p.sk.b + (int64_t)kvh * p.sk.h;
   const T* __restrict__ vg = static_cast<const T*>(p.v) + (int64_t)b * p.sv.b + (int64_t)kvh * p.sv.h;
 
-  // K^T and V^T as B operands: lane (h, key c) holds features 16 kc + 8 h ..
-  Range<T, false> range;
-  T* const kslot = reinterpret_cast<T*>(smem + NBUF * C::STAGE_BYTES) + 8 * tid;
-  Frag<T> kf[C::K_LDS ? 1 : KC], vf[KC];
-#pragma unroll
-  for (int kc = 0; kc < KC; ++kc) {
-    const Frag<T> f = live ? ld_frag_as<T, T>(kg + key * p.sk.r + 16 * kc + 8 * h, range) : zero_frag<T>();
-    if constexpr (C::K_LDS) *reinterpret_cast<Frag<T>*>(kslot + 8 * C::NT * kc) = f;
-    else kf[kc] = f;
-    vf[kc] = live ? ld_frag_as<T, T>(vg + key * p.sv.r + 16 * kc + 8 * h, range) : zero_frag<T>();
-  }
-  auto kfrag = [&](int kc) __attribute__((always_inline)) {
-    if constexpr (C::K_LDS) return lds_frag<T>(kslot + 8 * C::NT * kc);
-    else return kf[kc];
-  };
-
-  f32x16 dk[NDT], dv[NDT];
-#pragma unroll
-  for (int dt = 0; dt < NDT; ++dt)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) dk[dt][r] = dv[dt][r] = 0.0f;
-  wait_global_loads();
-
   // ---- the stream: for each head of the key head its query tiles.
   const int n_units = (int)((p.n_q + 31) / 32);
   const int2* const ranges = sa.q_range ? sa.q_range + (int64_t)b * n_units : nullptr;
@@ -193,6 +170,7 @@ __global__ __launch_bounds__(256, (ScoredKvTile<T, D>::OCC)) void scored_dkdv_ke
              static_cast<const T*>(p.d_o) + (int64_t)b * p.sdo.b + (int64_t)head_of(g_) * p.sdo.h, p.sdo.r,
              (int64_t)t_ * BQ, p.n_q, __builtin_amdgcn_readfirstlane(lds_addr(smem + buf * C::STAGE_BYTES)), wave);
   };
+  Range<T, false> range;
   Chunk8<T> stage[F32 ? C::CPT : 1];
   auto load_stage = [&](int g_, int t_) __attribute__((always_inline)) {
     if constexpr (F32) {
@@ -223,6 +201,33 @@ __global__ __launch_bounds__(256, (ScoredKvTile<T, D>::OCC)) void scored_dkdv_ke
       }
     }
   };
+
+  // The first tile is on its way while K and V are read.
+  if (g < g_end) {
+    load_rows(g, t);
+    if constexpr (!F32) copy_tile(g, t, 0);
+  }
+
+  // K^T and V^T as B operands: lane (h, key c) holds features 16 kc + 8 h ..
+  T* const kslot = reinterpret_cast<T*>(smem + NBUF * C::STAGE_BYTES) + 8 * tid;
+  Frag<T> kf[C::K_LDS ? 1 : KC], vf[KC];
+#pragma unroll
+  for (int kc = 0; kc < KC; ++kc) {
+    const Frag<T> f = live ? ld_frag_as<T, T>(kg + key * p.sk.r + 16 * kc + 8 * h, range) : zero_frag<T>();
+    if constexpr (C::K_LDS) *reinterpret_cast<Frag<T>*>(kslot + 8 * C::NT * kc) = f;
+    else kf[kc] = f;
+    vf[kc] = live ? ld_frag_as<T, T>(vg + key * p.sv.r + 16 * kc + 8 * h, range) : zero_frag<T>();
+  }
+  auto kfrag = [&](int kc) __attribute__((always_inline)) {
+    if constexpr (C::K_LDS) return lds_frag<T>(kslot + 8 * C::NT * kc);
+    else return kf[kc];
+  };
+
+  f32x16 dk[NDT], dv[NDT];
+#pragma unroll
+  for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) dk[dt][r] = dv[dt][r] = 0.0f;
 
   const int qrow = perm32(c);
   const float unit = sa.unit;
@@ -363,12 +368,9 @@ __global__ __launch_bounds__(256, (ScoredKvTile<T, D>::OCC)) void scored_dkdv_ke
 
   int buf = 0, g_bias = -1;
   if (g < g_end) {
-    load_rows(g, t);
     if constexpr (F32) {
       load_stage(g, t);
       store_stage(0);
-    } else {
-      copy_tile(g, t, 0);
     }
     store_rows(0);
   }
@@ -532,44 +534,8 @@ __global__ __launch_bounds__(256, (ScoredDqTile<T, D>::OCC)) void scored_dq_kern
   const int n_units = (int)((p.n_k + 31) / 32);
   DocTiles<BK / 32> docs(sa.k_range ? sa.k_range + (int64_t)b * n_units : nullptr, n_units, ids.x, ids.y);
 
-  const float unit = sa.unit;
-  const float slope = BIAS && sa.slopes ? sa.slopes[head] * (kLog2eF / unit) : 0.0f;
-  const int places = BIAS ? bias_places(sa) : 0;
-  const bool sums = BIAS && p.table_part;
-  // For the bias gradient: sums by place of each wave, and each wave's 32 x 64 skewed
-  // tile: dS of row c and key x at column x - c + 31, so that a column is a diagonal;
-  // the places that no pair has stay 0.
-  float* const bins = reinterpret_cast<float*>(lds_bias + bias_lds_bytes(sa, 1));
-  float* const my_bins = bins + wave * places;
-  float* const skew = bins + 4 * places + 2048 * wave;
-  if (BIAS && sa.table) {
-    fill_bias(sa, lds_bias, 1, head, tid, C::NT);
-    if (sums)
-      for (int x = tid; x < 4 * places + 8192; x += C::NT) bins[x] = 0.0f;
-  }
-
   const T* __restrict__ kg = static_cast<const T*>(p.k) + (int64_t)b * p.sk.b + (int64_t)kvh * p.sk.h;
   const T* __restrict__ vg = static_cast<const T*>(p.v) + (int64_t)b * p.sv.b + (int64_t)kvh * p.sv.h;
-  Range<T, false> range;
-  Frag<T> qf[KC], gf[KC];
-  {
-    const T* qg = static_cast<const T*>(p.q) + (int64_t)b * p.sq.b + (int64_t)head * p.sq.h + qi * p.sq.r;
-    const T* og = static_cast<const T*>(p.d_o) + (int64_t)b * p.sdo.b + (int64_t)head * p.sdo.h + qi * p.sdo.r;
-#pragma unroll
-    for (int kc = 0; kc < KC; ++kc) {
-      qf[kc] = live ? ld_frag_as<T, T>(qg + 16 * kc + 8 * h, range) : zero_frag<T>();
-      gf[kc] = live ? ld_frag_as<T, T>(og + 16 * kc + 8 * h, range) : zero_frag<T>();
-    }
-  }
-  f32x16 acc[NDT];
-#pragma unroll
-  for (int dt = 0; dt < NDT; ++dt)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) acc[dt][r] = 0.0f;
-  float far_lo = 0.0f, far_hi = 0.0f;
-  wait_global_loads();
-  __syncthreads();  // the bias is there
-
   constexpr int CPR = C::CPR;
   const TileCopy<std::conditional_t<F32, __bf16, T>, D, BK, false> copies(wave, lane, p.sk.r, p.sv.r);
   auto copy_tile = [&](int t, int buf) __attribute__((always_inline)) {
@@ -577,6 +543,7 @@ __global__ __launch_bounds__(256, (ScoredDqTile<T, D>::OCC)) void scored_dq_kern
       copies(kg, p.sk.r, vg, p.sv.r, (int64_t)t * BK, lim_hi,
              __builtin_amdgcn_readfirstlane(lds_addr(smem + buf * C::STAGE_BYTES)), wave);
   };
+  Range<T, false> range;
   Chunk8<T> stage[F32 ? C::CPT : 1];
   auto load_stage = [&](int t) __attribute__((always_inline)) {
     if constexpr (F32) {
@@ -605,6 +572,47 @@ __global__ __launch_bounds__(256, (ScoredDqTile<T, D>::OCC)) void scored_dq_kern
       }
     }
   };
+
+  // The first tile is on its way while the rest is set up.
+  const int64_t t_all = (lim_hi + BK - 1) / BK;
+  const int t_end = (int)(t_all * (part + 1) / p.dq_parts);
+  int t = docs.next((int)(t_all * part / p.dq_parts), t_end), buf = 0;
+  if constexpr (!F32)
+    if (t < t_end) copy_tile(t, 0);
+
+  const float unit = sa.unit;
+  const float slope = BIAS && sa.slopes ? sa.slopes[head] * (kLog2eF / unit) : 0.0f;
+  const int places = BIAS ? bias_places(sa) : 0;
+  const bool sums = BIAS && p.table_part;
+  // For the bias gradient: sums by place of each wave, and each wave's 32 x 64 skewed
+  // tile: dS of row c and key x at column x - c + 31, so that a column is a diagonal;
+  // the places that no pair has stay 0.
+  float* const bins = reinterpret_cast<float*>(lds_bias + bias_lds_bytes(sa, 1));
+  float* const my_bins = bins + wave * places;
+  float* const skew = bins + 4 * places + 2048 * wave;
+  if (BIAS && sa.table) {
+    fill_bias(sa, lds_bias, 1, head, tid, C::NT);
+    if (sums)
+      for (int x = tid; x < 4 * places + 8192; x += C::NT) bins[x] = 0.0f;
+  }
+
+  Frag<T> qf[KC], gf[KC];
+  {
+    const T* qg = static_cast<const T*>(p.q) + (int64_t)b * p.sq.b + (int64_t)head * p.sq.h + qi * p.sq.r;
+    const T* og = static_cast<const T*>(p.d_o) + (int64_t)b * p.sdo.b + (int64_t)head * p.sdo.h + qi * p.sdo.r;
+#pragma unroll
+    for (int kc = 0; kc < KC; ++kc) {
+      qf[kc] = live ? ld_frag_as<T, T>(qg + 16 * kc + 8 * h, range) : zero_frag<T>();
+      gf[kc] = live ? ld_frag_as<T, T>(og + 16 * kc + 8 * h, range) : zero_frag<T>();
+    }
+  }
+  f32x16 acc[NDT];
+#pragma unroll
+  for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) acc[dt][r] = 0.0f;
+  float far_lo = 0.0f, far_hi = 0.0f;
+  __syncthreads();  // the bias is there
 
   const int krow = perm32(c);
   const int64_t p_lo = pos0 + qw, p_hi = pos0 + w_last;  // the wave's positions
@@ -745,18 +753,13 @@ __global__ __launch_bounds__(256, (ScoredDqTile<T, D>::OCC)) void scored_dq_kern
     }
   };
 
-  const int64_t t_all = (lim_hi + BK - 1) / BK;
-  const int t_end = (int)(t_all * (part + 1) / p.dq_parts);
-  int t = docs.next((int)(t_all * part / p.dq_parts), t_end), buf = 0;
-  if (t < t_end) {
-    if constexpr (F32) {
+  if constexpr (F32) {
+    if (t < t_end) {
       load_stage(t);
       store_stage(0);
-    } else {
-      copy_tile(t, 0);
     }
+    __syncthreads();
   }
-  if constexpr (F32) __syncthreads();
   while (t < t_end) {
     const int tn = docs.next(t + 1, t_end);
     const bool masked = (int64_t)(t + 1) * BK > lim_lo;

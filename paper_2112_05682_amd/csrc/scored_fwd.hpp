@@ -114,10 +114,6 @@ __device__ __forceinline__ void stream_workgroup(const StreamParams& p, int bloc
   const int n_units = (int)((p.n_k + 31) / 32);
   DocTiles<UNITS> docs(sa.k_range ? sa.k_range + (int64_t)b0 * n_units : nullptr, n_units, ids.x, ids.y);
 
-  const float unit = sa.unit;
-  const float slope = BIAS && sa.slopes ? sa.slopes[head] * (kLog2eF / unit) : 0.0f;
-  if (BIAS && sa.table) fill_bias(sa, lds_bias, p.fold, head0, tid, C::NT);
-
   // ---- keys of this range: the visible tiles dealt evenly.
   const int all_tiles = (int)((lim_hi + BK - 1) / BK);
   const int per = (all_tiles + p.n_splits - 1) / p.n_splits;
@@ -126,25 +122,6 @@ __device__ __forceinline__ void stream_workgroup(const StreamParams& p, int bloc
   const int64_t kb = p.batches > 1 ? 0 : (int64_t)b0;
   const T* __restrict__ kg = static_cast<const T*>(p.k) + kb * p.sk.b + (int64_t)kvh * p.sk.h;
   const T* __restrict__ vg = static_cast<const T*>(p.v) + kb * p.sv.b + (int64_t)kvh * p.sv.h;
-
-  // ---- Q^T as B operands: lane (h, row c) holds features 16 kc + 8 h ..
-  Range<T, false> range;
-  Frag<T> qf[KC];
-  {
-    const T* qg = static_cast<const T*>(p.q) + (int64_t)b * p.sq.b + (int64_t)head * p.sq.h + qi * p.sq.r;
-#pragma unroll
-    for (int kc = 0; kc < KC; ++kc)
-      qf[kc] = lim > 0 ? ld_frag_as<T, T>(qg + 16 * kc + 8 * h, range) : zero_frag<T>();
-  }
-
-  f32x16 acc[NDT];
-#pragma unroll
-  for (int dt = 0; dt < NDT; ++dt)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) acc[dt][r] = 0.0f;
-  float m_ref = -INFINITY, l_run = 0.0f;
-  wait_global_loads();
-  __syncthreads();  // the bias is there
 
   // ---- staging.  16-bit: copies of 1 KiB, rows past the last visible key repeat
   // it (finite, and masked); with RW = 1 each wave copies its own keys.
@@ -156,6 +133,7 @@ __device__ __forceinline__ void stream_workgroup(const StreamParams& p, int bloc
       copies(kg, p.sk.r, vg, p.sv.r, (int64_t)t * BK, lim_hi,
              __builtin_amdgcn_readfirstlane(lds_addr(smem + buf * C::STAGE_BYTES)), wave);
   };
+  Range<T, false> range;
   Chunk8<T> stage[F32 ? C::CPT : 1];
   auto load_stage = [&](int t) __attribute__((always_inline)) {
     if constexpr (F32) {
@@ -185,6 +163,32 @@ __device__ __forceinline__ void stream_workgroup(const StreamParams& p, int bloc
       }
     }
   };
+
+  // The first tile is on its way while the rest is set up.
+  int t = docs.next(t0, t1), buf = 0;
+  if constexpr (!F32)
+    if (t < t1) copy_tile(t, 0);
+
+  const float unit = sa.unit;
+  const float slope = BIAS && sa.slopes ? sa.slopes[head] * (kLog2eF / unit) : 0.0f;
+  if (BIAS && sa.table) fill_bias(sa, lds_bias, p.fold, head0, tid, C::NT);
+
+  // ---- Q^T as B operands: lane (h, row c) holds features 16 kc + 8 h ..
+  Frag<T> qf[KC];
+  {
+    const T* qg = static_cast<const T*>(p.q) + (int64_t)b * p.sq.b + (int64_t)head * p.sq.h + qi * p.sq.r;
+#pragma unroll
+    for (int kc = 0; kc < KC; ++kc)
+      qf[kc] = lim > 0 ? ld_frag_as<T, T>(qg + 16 * kc + 8 * h, range) : zero_frag<T>();
+  }
+
+  f32x16 acc[NDT];
+#pragma unroll
+  for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) acc[dt][r] = 0.0f;
+  float m_ref = -INFINITY, l_run = 0.0f;
+  __syncthreads();  // the bias is there
 
   const int krow = perm32(c);
 
@@ -343,15 +347,12 @@ __device__ __forceinline__ void stream_workgroup(const StreamParams& p, int bloc
   };
 
   // ---- the loop over the visible tiles of this range.
-  int t = docs.next(t0, t1), buf = 0;
   if constexpr (F32) {
     if (t < t1) {
       load_stage(t);
       store_stage(0);
     }
     __syncthreads();
-  } else {
-    if (t < t1) copy_tile(t, 0);
   }
   while (t < t1) {
     const int tn = docs.next(t + 1, t1);
