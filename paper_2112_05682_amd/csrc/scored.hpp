@@ -393,16 +393,17 @@ struct ScoredBwdParams {
 
 // Into how many parts dK/dV workgroups split their heads and their queries, and dQ
 // workgroups their keys, where the tiles alone would leave places on the chip empty
-// (the parts' float32 sums are added afterwards, in order): as many as fill the
-// chip's places, twice over with the causal mask, whose tiles differ in length.  Heads
-// before queries, as a part of a head reads the same keys again.  Forward + backward
-// in us with 1 / 2 / 4 / 8 / 16 parts of dK/dV (dQ whole), and as the rule has it:
-// bf16 d = 128 causal 2x16 heads on 4, 4096 (256 workgroups) 1380 / 1022 / 865 / 925 /
-// 1042, rule 4: 862; 3x2 on 1, 3761 (90) 644 / 443 / 347 / 303 / 335, rule 11, dQ 5: 248;
-// 3x24 on 3, 897 (72) 468 / 296 / 209 / 175 / 189, rule 14: 179; d = 64 4x12, 1999 (768)
-// 219 / 234 / 275, rule 1, dQ 1: 207; 4x16, 4096 (2048) 887 / 994; float32 d = 64 2x8 on 4,
-// 700 (48) 219 / 168 / 142 / 135 / 142, rule 10, dQ 6: 122; d = 128 2x4 on 2, 1000 (32) 743
-// / 495 / 374 / 317 / 312, rule 16, dQ 8: 204.
+// (the parts' float32 sums are added afterwards, in order).  The two kinds run in one
+// launch, so each is to fill half the chip's places; with the causal mask, whose tiles
+// differ in length, all of them, 16-bit one and a half times over.  Heads before queries, as
+// a part of a head reads the same keys again, and a number of heads that leaves
+// no part more than another.  Backward in us at 1 / 0.75 / 0.5 of twice that (causal 16-bit:
+// of 1.33 times), bf16 d = 64 2x8 heads, 1000 unmasked 56 / 55 / 45; 4x12, 1999 causal 156 /
+// 140 / 140; d = 128 4x8, 1000 unmasked 128 / 100 / 100; causal 3x2 on 1, 3761 156 / 145 / 154;
+// 3x24 on 3, 897 120 / 120 / 145; 10x8 on 2, 1309 210 / 204 / 199; float32 d = 128 2x4 on 2,
+// 1000 causal 148 / 136 / 116.  Forward + backward without parts and with them: causal
+// bf16 d = 128 2x16 on 4, 4096 1380 / 862, 3x2 on 1, 3761 644 / 248; float32 d = 64 2x8 on 4, 700
+// 219 / 122.
 struct BwdParts {
   int kv_heads, kv_queries, dq;
 };
@@ -410,16 +411,19 @@ inline BwdParts bwd_parts(bool is16, bool causal, int d, int64_t n_q, int64_t n_
                           int64_t heads_kv) {
   const int64_t G = heads / heads_kv, kv_wgs = batch * heads_kv * ((n_k + 127) / 128), q_wgs = batch * heads * ((n_q + 127) / 128);
   const int64_t kv_places = is16 ? 512 : 256, q_places = is16 || d == 64 ? 512 : 256;
-  BwdParts r = {1, 1, 1};
-  int64_t want = kv_places * (causal ? 2 : 1) / kv_wgs;
+  const double fill = !causal ? 0.5 : (is16 ? 1.5 : 1.0);
   const int64_t q_tiles = (n_q + 127) / 128, k_tiles = (n_k + 127) / 128;
+  BwdParts r = {1, 1, 1};
+  int64_t want = (int64_t)(fill * (double)kv_places / (double)kv_wgs);
   if (want > 1) {
-    r.kv_heads = (int)(want < G ? want : G);
-    int64_t pq = want / r.kv_heads;
+    int64_t ph = want < G ? want : G;
+    while (G % ph) ++ph;
+    int64_t pq = want / ph;
     if (pq > q_tiles) pq = q_tiles;
+    r.kv_heads = (int)ph;
     r.kv_queries = pq < 1 ? 1 : (int)pq;
   }
-  want = q_places * (causal ? 2 : 1) / q_wgs;
+  want = (int64_t)(fill * (double)q_places / (double)q_wgs);
   if (want > k_tiles) want = k_tiles;
   if (want > 1) r.dq = (int)want;
   return r;

@@ -81,8 +81,9 @@ struct ScoredKvTile {
   static_assert(F32 || NBUF == 2, "asynchronous copies need two stages");
 };
 
+// Workgroup `block` of n_blocks.
 template <typename T, int D, bool CAP, bool BIAS>
-__global__ __launch_bounds__(256, (ScoredKvTile<T, D>::OCC)) void scored_dkdv_kernel(ScoredBwdParams p) {
+__device__ __forceinline__ void dkdv_workgroup(const ScoredBwdParams& p, int block, int n_blocks) {
   using C = ScoredKvTile<T, D>;
   using LE = typename Planes<T>::E;
   constexpr bool F32 = C::F32;
@@ -96,7 +97,7 @@ __global__ __launch_bounds__(256, (ScoredKvTile<T, D>::OCC)) void scored_dkdv_ke
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   const int h = lane >> 5, c = lane & 31;
 
-  const TileItem item = tile_item(blockIdx.x, gridDim.x, p.n_ktiles, sa.causal ? p.tile_order : 0);
+  const TileItem item = tile_item(block, n_blocks, p.n_ktiles, sa.causal ? p.tile_order : 0);
   const int b = item.group % p.n_b, kvh = item.group / p.n_b % p.heads_kv;
   // This part's heads and its share of the tiles of queries.
   const int part = item.group / (p.n_b * p.heads_kv);
@@ -485,7 +486,7 @@ struct ScoredDqTile {
 };
 
 template <typename T, int D, bool CAP, bool BIAS>
-__global__ __launch_bounds__(256, (ScoredDqTile<T, D>::OCC)) void scored_dq_kernel(ScoredBwdParams p) {
+__device__ __forceinline__ void dq_workgroup(const ScoredBwdParams& p, int block, int n_blocks) {
   using C = ScoredDqTile<T, D>;
   using LE = typename Planes<T>::E;
   constexpr bool F32 = C::F32;
@@ -500,7 +501,7 @@ __global__ __launch_bounds__(256, (ScoredDqTile<T, D>::OCC)) void scored_dq_kern
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   const int h = lane >> 5, c = lane & 31;
 
-  const TileItem item = tile_item(blockIdx.x, gridDim.x, p.n_qtiles, sa.causal ? p.tile_order : 0);
+  const TileItem item = tile_item(block, n_blocks, p.n_qtiles, sa.causal ? p.tile_order : 0);
   const int qtile = sa.causal ? p.n_qtiles - 1 - item.tile : item.tile;
   // Heads that share a key head are neighbours, then batches.
   const int gi = item.group / p.heads_per_kv;
@@ -865,6 +866,23 @@ __global__ __launch_bounds__(256, (ScoredDqTile<T, D>::OCC)) void scored_dq_kern
   }
 }
 
+// dK/dV (the first n_kv workgroups) and dQ in one launch, where each fills what the
+// other leaves of the chip.  PARTS 1 and 2, a launch each, for larger float32 grids at
+// d = 64, where dQ alone has two workgroups per CU and dK/dV one.  Backward in us, two
+// launches / one: bf16 d = 64 4x16 heads, 4096 causal 676 / 657, 16x12, 512 121 / 99, 15x15
+// on 5, 1199 518 / 497; d = 128 2x16 on 4, 4096 causal 673 / 655, 3x24 on 3, 897 129 / 121,
+// 2x32 on 8, 4096 1032 / 1050; float32 d = 64 1x4, 64 39 / 24, 2x8 on 4, 700 75 / 79, 4x8, 2000
+// 381 / 436; d = 128 4x8, 2000 952 / 929.
+template <typename T, int D, bool CAP, bool BIAS, int PARTS>
+__global__ __launch_bounds__(256, PARTS == 2 ? (ScoredDqTile<T, D>::OCC) : (ScoredKvTile<T, D>::OCC))
+void scored_bwd_kernel(ScoredBwdParams p, int n_kv) {
+  const int block = (int)blockIdx.x;
+  if constexpr (PARTS & 1)
+    if (block < n_kv) dkdv_workgroup<T, D, CAP, BIAS>(p, block, n_kv);
+  if constexpr (PARTS & 2)
+    if (block >= n_kv) dq_workgroup<T, D, CAP, BIAS>(p, block - n_kv, (int)gridDim.x - n_kv);
+}
+
 // The parts' sums, added in order, scaled and rounded: blocks of rows of dK, of dV, of
 // dQ; a thread per row and 4 features.
 template <typename T, int D>
@@ -908,22 +926,31 @@ static hipError_t launch_scored_bwd_kernels(const ScoredBwdParams& p, hipStream_
   using K = ScoredKvTile<T, D>;
   using Q = ScoredDqTile<T, D>;
   ScoredBwdParams a = p;
-  void* args[] = {&a};
   a.n_ktiles = (int)((p.n_k + K::BKG - 1) / K::BKG);
   a.n_qtiles = (int)((p.n_q + Q::ROWS - 1) / Q::ROWS);
-  const int bias = bias_lds_bytes(p.s, 1);
+  const int64_t kv_wgs = p.dk ? (int64_t)a.n_ktiles * p.n_b * p.heads_kv * p.kv_heads_parts * p.kv_query_parts : 0;
+  const int64_t q_wgs = p.dq ? (int64_t)a.n_qtiles * p.n_b * p.s.heads * p.dq_parts : 0;
+  const int bias = bias_lds_bytes(p.s, 1), bins = p.table_part ? (4 * bias_places(p.s) + 8192) * 4 : 0;
+  const int kv_lds = K::LDS_BYTES + bias, q_lds = Q::LDS_BYTES + bias + bins;
+  int n_kv = (int)kv_wgs;
+  void* args[] = {&a, &n_kv};
+  static_assert(Q::OCC >= K::OCC, "one launch has dK/dV's registers");
+  auto launch = [&](auto parts, int64_t grid, int lds) {
+    return hipLaunchKernel(reinterpret_cast<const void*>(scored_bwd_kernel<T, D, CAP, BIAS, decltype(parts)::value>),
+                           dim3((unsigned)grid), dim3(256), args, lds, stream);
+  };
   hipError_t e = hipSuccess;
-  if (p.dk) {
-    e = hipLaunchKernel(reinterpret_cast<const void*>(scored_dkdv_kernel<T, D, CAP, BIAS>),
-                        dim3((unsigned)((int64_t)a.n_ktiles * p.n_b * p.heads_kv * p.kv_heads_parts * p.kv_query_parts)), dim3(K::NT), args, K::LDS_BYTES + bias,
-                        stream);
-    if (e != hipSuccess) return e;
+  bool one = true;
+  if constexpr (Q::OCC > K::OCC) {
+    one = kv_wgs && q_wgs && kv_wgs + q_wgs <= 256;
+    if (!one && kv_wgs) e = launch(std::integral_constant<int, 1>{}, kv_wgs, kv_lds);
+    n_kv = one ? n_kv : 0;
+    if (!one && q_wgs && e == hipSuccess) e = launch(std::integral_constant<int, 2>{}, q_wgs, q_lds);
   }
-  if (!p.dq) return launch_scored_sum<T, D>(a, stream);
-  const int bins = p.table_part ? (4 * bias_places(p.s) + 8192) * 4 : 0;
-  e = hipLaunchKernel(reinterpret_cast<const void*>(scored_dq_kernel<T, D, CAP, BIAS>),
-                      dim3((unsigned)((int64_t)a.n_qtiles * p.n_b * p.s.heads * p.dq_parts)), dim3(Q::NT), args,
-                      Q::LDS_BYTES + bias + bins, stream);
+  if (one) {
+    const int lds = !q_wgs || (kv_wgs && kv_lds > q_lds) ? kv_lds : q_lds;
+    e = launch(std::integral_constant<int, 3>{}, kv_wgs + q_wgs, lds);
+  }
   if (e == hipSuccess && p.table_part) e = launch_scored_table(a, stream);
   return e != hipSuccess ? e : launch_scored_sum<T, D>(a, stream);
 }
