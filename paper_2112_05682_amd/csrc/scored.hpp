@@ -299,6 +299,24 @@ __device__ __forceinline__ int4 workgroup_ids(int id, int wave, int lane, int4* 
                    __builtin_amdgcn_readfirstlane(a.z), 0);
 }
 
+// Hides the pairs of other documents than the lane's.  mine: the ids of the 32 tokens
+// across, one on each lane of a half, which go by way of 32 words of LDS of this wave's
+// own: a write and 4 reads of 16 bytes that all lanes of a half share, a group at a
+// time (registers).
+__device__ __forceinline__ void hide_documents(f32x16& s, int doc, int mine, int* lds, int lane) {
+  typedef int i32x4 __attribute__((ext_vector_type(4)));
+  if (lane < 32) lds[lane] = mine;
+  const int* at = lds + 8 * (lane >> 5);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const i32x4 x = *reinterpret_cast<const i32x4*>(at + 16 * (j >> 1) + 4 * (j & 1));
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (x[e] != doc) s[4 * j + e] = -INFINITY;
+    __builtin_amdgcn_sched_barrier(0);
+  }
+}
+
 // Zeroes the rows of two staged tiles whose tokens have no document (the tiles' rows
 // are tokens r0 .., from `end` on the last one before it again), so that whatever they
 // hold meets weights of 0 as a number.  nt threads, for rows [first, first + rows); the caller synchronises.

@@ -59,6 +59,12 @@ __global__ __launch_bounds__(256) void scored_bwd_pre_kernel(ScoredBwdParams p) 
   }
 }
 
+// 1 - tanh^2 of a score that is still the tanh, or hidden (-inf, whose weight is 0).
+__device__ __forceinline__ float cap_grad(float t) {
+  t = fmaxf(t, -1.0f);
+  return fmaf(-t, t, 1.0f);
+}
+
 // ------------------------------------------------------------------- dK, dV
 template <typename T, int D>
 struct ScoredKvTile {
@@ -74,7 +80,7 @@ struct ScoredKvTile {
   static constexpr bool K_LDS = !F32 && D == 128;
   static constexpr int KSLOT_BYTES = K_LDS ? NT * (D / 16) * 16 : 0;
   static constexpr int kBiasMax = 4 * (2 * kMaxBiasSpan + 1 + 2 * kPad) + 16;
-  static constexpr int NBUF = 2 * STAGE_BYTES + KSLOT_BYTES + kBiasMax <= 160 * 1024 / OCC - 64 ? 2 : 1;
+  static constexpr int NBUF = 2 * STAGE_BYTES + KSLOT_BYTES + kBiasMax <= 160 * 1024 / OCC - 1280 ? 2 : 1;
   static constexpr int LDS_BYTES = NBUF * STAGE_BYTES + KSLOT_BYTES;
   static constexpr int CPR = D / 8, CHUNKS = 2 * BQ * CPR, CPT = CHUNKS / NT;
   static_assert(CHUNKS % NT == 0, "tile shapes");
@@ -87,11 +93,13 @@ __device__ __forceinline__ void dkdv_workgroup(const ScoredBwdParams& p, int blo
   using C = ScoredKvTile<T, D>;
   using LE = typename Planes<T>::E;
   constexpr bool F32 = C::F32;
+  constexpr bool KEEP = CAP && (BIAS || D == 64);  // 1 - tanh^2 is kept, else (registers) made again from the score
   constexpr int BQ = C::BQ, QS = C::QS, KC = D / 16, NDT = D / 32, NBUF = C::NBUF;
 
   extern __shared__ __align__(16) unsigned char smem[];
   unsigned char* const lds_bias = smem + C::LDS_BYTES;
   __shared__ int4 wave_ids[4];
+  __shared__ __align__(16) int tile_ids[4][32];
 
   const ScoreArgs& sa = p.s;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
@@ -280,12 +288,12 @@ __device__ __forceinline__ void dkdv_workgroup(const ScoredBwdParams& p, int blo
           __builtin_amdgcn_sched_barrier(0);
         }
       }
-      float grad[CAP ? 16 : 1];  // 1 - tanh^2
+      float grad[KEEP ? 16 : 1];
       if constexpr (CAP) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           s[r] = cap_tanh<T>(sa, s[r]);
-          grad[r] = fmaf(-s[r], s[r], 1.0f);
+          if constexpr (KEEP) grad[r] = fmaf(-s[r], s[r], 1.0f);
         }
       }
       float add = 0.0f;  // what every pair gets
@@ -326,11 +334,7 @@ __device__ __forceinline__ void dkdv_workgroup(const ScoredBwdParams& p, int blo
       if (by_doc) {
         asm volatile("");
         const int mine = q0 + c < p.n_q ? sa.q_doc[(int64_t)b * p.n_q + q0 + c] : -1;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int id = __shfl(mine, permuted_row(r, h));
-          if (id != doc) s[r] = -INFINITY;
-        }
+        hide_documents(s, doc, mine, tile_ids[wave], lane);
       }
       // P, dS and dX, rounded to the operands of the products with dO and Q.
       Frag<T> pf[2], sf[2];
@@ -345,7 +349,8 @@ __device__ __forceinline__ void dkdv_workgroup(const ScoredBwdParams& p, int blo
             const int r = 8 * m + 4 * j + e;
             x[4 * j + e] = fast_exp2(fmaf(s[r], unit, BIAS ? fmaf(add, unit, -l2[e]) : -l2[e]));
             y[4 * j + e] = x[4 * j + e] * dp[r];
-            if constexpr (CAP) y[4 * j + e] *= grad[r];
+            if constexpr (KEEP) y[4 * j + e] *= grad[r];
+            else if constexpr (CAP) y[4 * j + e] *= cap_grad(s[r]);
           }
         }
         pf[m] = to_frag<T>(x);
@@ -478,7 +483,7 @@ struct ScoredDqTile {
   static constexpr int OCC = F32 && D == 128 ? 1 : 2;
   // The bias by place; its gradient takes 4 waves' sums by place and 32 KiB more.
   static constexpr int kBiasMax = 4 * (2 * kMaxBiasSpan + 1 + 2 * kPad) + 16;
-  static constexpr int NBUF = 2 * STAGE_BYTES + 5 * kBiasMax + 32768 <= 160 * 1024 - 256 ? 2 : 1;
+  static constexpr int NBUF = 2 * STAGE_BYTES + 5 * kBiasMax + 32768 <= 160 * 1024 - 1280 ? 2 : 1;
   static constexpr int LDS_BYTES = NBUF * STAGE_BYTES;
   static constexpr int CPR = D / 8, CHUNKS = 2 * BK * CPR, CPT = CHUNKS / NT;
   static_assert(CHUNKS % NT == 0, "tile shapes");
@@ -490,11 +495,13 @@ __device__ __forceinline__ void dq_workgroup(const ScoredBwdParams& p, int block
   using C = ScoredDqTile<T, D>;
   using LE = typename Planes<T>::E;
   constexpr bool F32 = C::F32;
+  constexpr bool KEEP = CAP && (BIAS || D == 64);  // 1 - tanh^2 is kept, else (registers) made again from the score
   constexpr int BK = C::BK, KC = D / 16, NKT = BK / 32, NDT = D / 32, NBUF = C::NBUF;
 
   extern __shared__ __align__(16) unsigned char smem[];
   unsigned char* const lds_bias = smem + C::LDS_BYTES;
   __shared__ int4 wave_ids[4];
+  __shared__ __align__(16) int tile_ids[4][32];
   __shared__ float far_sums[8];
 
   const ScoreArgs& sa = p.s;
@@ -655,12 +662,12 @@ __device__ __forceinline__ void dq_workgroup(const ScoredBwdParams& p, int block
           __builtin_amdgcn_sched_barrier(0);
         }
       }
-      float grad[CAP ? 16 : 1];
+      float grad[KEEP ? 16 : 1];
       if constexpr (CAP) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           s[r] = cap_tanh<T>(sa, s[r]);
-          grad[r] = fmaf(-s[r], s[r], 1.0f);
+          if constexpr (KEEP) grad[r] = fmaf(-s[r], s[r], 1.0f);
         }
       }
       float add = 0.0f;  // what every pair gets
@@ -701,11 +708,7 @@ __device__ __forceinline__ void dq_workgroup(const ScoredBwdParams& p, int block
       if (by_doc) {
         asm volatile("");
         const int mine = k0 + c < p.n_k ? sa.k_doc[(int64_t)b * p.n_k + k0 + c] : -1;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int id = __shfl(mine, permuted_row(r, h));
-          if (id != doc) s[r] = -INFINITY;
-        }
+        hide_documents(s, doc, mine, tile_ids[wave], lane);
       }
       const float neg = BIAS ? fmaf(add, unit, -l2) : -l2;
 #pragma unroll
@@ -735,7 +738,10 @@ __device__ __forceinline__ void dq_workgroup(const ScoredBwdParams& p, int block
       }
       if constexpr (CAP)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) dp[r] *= grad[r];
+        for (int r = 0; r < 16; ++r) {
+          if constexpr (KEEP) dp[r] *= grad[r];
+          else dp[r] *= cap_grad(s[r]);
+        }
       Frag<T> sf[2];
 #pragma unroll
       for (int m = 0; m < 2; ++m) {

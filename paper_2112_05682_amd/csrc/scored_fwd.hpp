@@ -35,7 +35,7 @@ struct StreamTile {
   static constexpr int CPR = D / 8, CHUNKS = 2 * BK * CPR, CPT = CHUNKS / NT;
   static_assert(CHUNKS % NT == 0 && BKW % 32 == 0, "tile shapes");
   static_assert(F32 || NBUF == 2, "asynchronous copies need two stages");
-  static_assert((LDS_BYTES + kBiasMax) * OCC <= 160 * 1024, "LDS");
+  static_assert((LDS_BYTES + kBiasMax + 1280) * OCC <= 160 * 1024, "LDS");
 };
 
 // Workgroup `block` of n_blocks.
@@ -49,6 +49,7 @@ __device__ __forceinline__ void stream_workgroup(const StreamParams& p, int bloc
   extern __shared__ __align__(16) unsigned char smem[];
   unsigned char* const lds_bias = smem + C::LDS_BYTES;
   __shared__ int4 wave_ids[4];
+  __shared__ __align__(16) int tile_ids[4][32];
 
   const ScoreArgs& sa = p.s;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
@@ -296,11 +297,7 @@ __device__ __forceinline__ void stream_workgroup(const StreamParams& p, int bloc
       for (int kt = 0; kt < NKT; ++kt) {
         const int64_t key = k0 + 32 * kt + c;
         const int mine = key < p.n_k ? sa.k_doc[(int64_t)b0 * p.n_k + key] : -1;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int id = __shfl(mine, permuted_row(r, h));
-          if (id != doc) s[kt][r] = -INFINITY;
-        }
+        hide_documents(s[kt], doc, mine, tile_ids[wave], lane);
       }
     }
 
@@ -577,7 +574,7 @@ static hipError_t launch_stream_kernel(const StreamParams& p, hipStream_t stream
   q.n_rtiles = (int)((p.group_rows + C::ROWS - 1) / C::ROWS);
   const int lds = C::LDS_BYTES + bias_lds_bytes(p.s, p.fold);
   const int64_t grid = (int64_t)q.n_rtiles * p.n_groups * p.n_splits;
-  if (grid < 1 || grid >= ((int64_t)1 << 31) || lds > 160 * 1024 - 64) return hipErrorInvalidValue;
+  if (grid < 1 || grid >= ((int64_t)1 << 31) || lds > 160 * 1024 - 1280) return hipErrorInvalidValue;
   void* args[] = {&q};
   return hipLaunchKernel(reinterpret_cast<const void*>(scored_stream_kernel<T, D, RW, CAP, BIAS>), dim3((unsigned)grid),
                          dim3(C::NT), args, lds, stream);
