@@ -29,6 +29,8 @@
 
 namespace mea {
 
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+
 constexpr int kMaxSideBuckets = 64;  // MEA_MAX_SIDE_BUCKETS
 constexpr int kMaxBiasSpan = 512;    // MEA_MAX_BIAS_SPAN
 constexpr float kLog2eF = 1.4426950408889634f, kLn2F = 0.6931471805599453f;

@@ -336,39 +336,72 @@ __device__ __forceinline__ void dkdv_workgroup(const ScoredBwdParams& p, int blo
         const int mine = q0 + c < p.n_q ? sa.q_doc[(int64_t)b * p.n_q + q0 + c] : -1;
         hide_documents(s, doc, mine, tile_ids[wave], lane);
       }
-      // P, dS and dX, rounded to the operands of the products with dO and Q.
-      Frag<T> pf[2], sf[2];
+      // dV^T += dO^T P and dK^T += Q^T dX, P and dX rounded to their operands.
+      const float base = BIAS ? add * unit : 0.0f;
+      auto weight = [&](int r, float l2, float& x, float& y) __attribute__((always_inline)) {
+        x = fast_exp2(fmaf(s[r], unit, BIAS ? base - l2 : -l2));
+        y = x * dp[r];
+        if constexpr (KEEP) y *= grad[r];
+        else if constexpr (CAP) y *= cap_grad(s[r]);
+      };
+      if constexpr (F32) {
+        Frag<T> pf[2], sf[2];
 #pragma unroll
-      for (int m = 0; m < 2; ++m) {
-        float x[8], y[8];
+        for (int m = 0; m < 2; ++m) {
+          float x[8], y[8];
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const f32x4 l2 = *reinterpret_cast<const f32x4*>(lse_s + 16 * m + 4 * j);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int r = 8 * m + 4 * j + e;
-            x[4 * j + e] = fast_exp2(fmaf(s[r], unit, BIAS ? fmaf(add, unit, -l2[e]) : -l2[e]));
-            y[4 * j + e] = x[4 * j + e] * dp[r];
-            if constexpr (KEEP) y[4 * j + e] *= grad[r];
-            else if constexpr (CAP) y[4 * j + e] *= cap_grad(s[r]);
-          }
+          for (int e = 0; e < 8; ++e) weight(8 * m + e, lse_s[16 * m + e], x[e], y[e]);
+          pf[m] = to_frag<T>(x);
+          sf[m] = to_frag<T>(y);
         }
-        pf[m] = to_frag<T>(x);
-        sf[m] = to_frag<T>(y);
-      }
-      // dV^T += dO^T P and dK^T += Q^T dX.
 #pragma unroll
-      for (int m = 0; m < 2; ++m)
+        for (int m = 0; m < 2; ++m)
 #pragma unroll
-        for (int dt = 0; dt < NDT; ++dt) {
-          if constexpr (F32) {
+          for (int dt = 0; dt < NDT; ++dt) {
             dv[dt] = mma(lds_col_frag_planes<T>(ot32, C::TILE, C::RS, 16 * m, 32 * dt, lane), pf[m], dv[dt]);
             dk[dt] = mma(lds_col_frag_planes<T>(qt32, C::TILE, C::RS, 16 * m, 32 * dt, lane), sf[m], dk[dt]);
-          } else {
-            dv[dt] = mma(col_frag<T, D>(ot, 16 * m, 32 * dt, lane), pf[m], dv[dt]);
-            dk[dt] = mma(col_frag<T, D>(qt, 16 * m, 32 * dt, lane), sf[m], dk[dt]);
           }
+      } else {
+        // The second 16 rows' weights are made between the first ones' products, a share
+        // a step, and each step's fragments are read one step ahead.
+        typedef uint32_t u32x4w __attribute__((ext_vector_type(4)));
+        constexpr int PER = 8 / NDT;
+        u32x4w pw, dw;
+        auto pair = [&](int m, int e) __attribute__((always_inline)) {
+          const f32x2 l2 = *reinterpret_cast<const f32x2*>(lse_s + 16 * m + e);
+          float x0, y0, x1, y1;
+          weight(8 * m + e, l2[0], x0, y0);
+          weight(8 * m + e + 1, l2[1], x1, y1);
+          pw[e / 2] = pack2<T>(x0, x1);
+          dw[e / 2] = pack2<T>(y0, y1);
+        };
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) pair(0, e);
+        Frag<T> pa = __builtin_bit_cast(Frag<T>, pw), da = __builtin_bit_cast(Frag<T>, dw);
+        Frag<T> bo = col_frag<T, D>(ot, 0, 0, lane), bq = col_frag<T, D>(qt, 0, 0, lane);
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+#pragma unroll
+          for (int dt = 0; dt < NDT; ++dt) {
+            const bool last = dt + 1 == NDT;
+            Frag<T> bo_n = bo, bq_n = bq;
+            if (!last || m == 0) {
+              bo_n = col_frag<T, D>(ot, 16 * (last ? m + 1 : m), last ? 0 : 32 * (dt + 1), lane);
+              bq_n = col_frag<T, D>(qt, 16 * (last ? m + 1 : m), last ? 0 : 32 * (dt + 1), lane);
+            }
+            dv[dt] = mma(bo, pa, dv[dt]);
+            dk[dt] = mma(bq, da, dk[dt]);
+            if (m == 0)
+#pragma unroll
+              for (int e = PER * dt; e < PER * dt + PER; e += 2) pair(1, e);
+            bo = bo_n;
+            bq = bq_n;
+            __builtin_amdgcn_sched_barrier(0);
+          }
+          pa = __builtin_bit_cast(Frag<T>, pw);
+          da = __builtin_bit_cast(Frag<T>, dw);
         }
+      }
     }
   };
 
