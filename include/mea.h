@@ -243,7 +243,7 @@ typedef struct {
   const int32_t* q_doc;      /* DEVICE int32 [B, n_q], contiguous; NULL with k_doc: no documents */
   const int32_t* k_doc;      /* DEVICE int32 [B, n_k] */
   const int32_t* prefix_len; /* DEVICE int32 [B], with causal only; or NULL */
-  const int32_t* q_pos;      /* DEVICE int32 [B], negative values read as 0; or NULL: 0 */
+  const int32_t* q_pos;      /* DEVICE int32 [B], negative values read as 0, q_pos + n_q below 2^31; or NULL: 0 */
 } mea_score;
 
 /* Bytes of device workspace of the two calls below (partial sums where the keys
@@ -258,7 +258,7 @@ mea_status mea_scored_attention_fwd(const mea_problem* p, const mea_score* s, co
                                     size_t workspace_bytes, hipStream_t stream);
 
 /* Backward; o, o_lo, d_o, lse, dq, dk and dv as in mea_attention_bwd.  d_table
- * ([buckets, H] in table_dtype, 4-byte aligned, or NULL) gets the bias's gradient
+ * ([buckets, H] in table_dtype, or NULL) gets the bias's gradient
  *   sum over batches and pairs of the bucket of w_ij (do_i . v_j - D_i)
  * and needs dq.  The same sums in the same order on every call. */
 mea_status mea_scored_attention_bwd(const mea_problem* p, const mea_score* s, const void* q, const void* k,

@@ -16,6 +16,8 @@ using mea::StreamParams;
 static_assert(mea::kMaxSideBuckets == MEA_MAX_SIDE_BUCKETS && mea::kMaxBiasSpan == MEA_MAX_BIAS_SPAN, "limits");
 
 bool aligned4(const void* p) { return ((uintptr_t)p & 3u) == 0; }
+// Whether a table's address is a multiple of its elements' size.
+bool table_aligned(const void* p, int32_t dtype) { return (uintptr_t)p % elem_size(dtype) == 0; }
 int64_t kv_heads_of(const mea_problem* p, int64_t given) { return given ? given : p->heads; }
 
 mea_status check_base(const mea_problem* p, int64_t kv_heads) {
@@ -34,13 +36,13 @@ mea_status check_score(const mea_problem* p, const mea_score* s) {
   if (!(s->softcap >= 0.0f) || !isfinite(s->softcap)) return MEA_ERR_INVALID_ARG;
   if (s->softcap > 0.0f && !(s->softcap * kLog2e > 0.0f && isfinite(s->softcap * kLog2e) && isfinite(2.0f * kLog2e * p->scale / s->softcap)))
     return MEA_ERR_INVALID_ARG;
-  if (!aligned4(s->slopes) || !aligned4(s->q_doc) || !aligned4(s->k_doc) || !aligned4(s->prefix_len) || !aligned4(s->q_pos) ||
-      !aligned4(s->table))
+  if (!aligned4(s->slopes) || !aligned4(s->q_doc) || !aligned4(s->k_doc) || !aligned4(s->prefix_len) || !aligned4(s->q_pos))
     return MEA_ERR_INVALID_ARG;
   if ((s->q_doc == nullptr) != (s->k_doc == nullptr)) return MEA_ERR_INVALID_ARG;
   if (s->prefix_len && !p->causal) return MEA_ERR_INVALID_ARG;
   if (s->table) {
     if (s->table_dtype != MEA_F32 && s->table_dtype != MEA_F16 && s->table_dtype != MEA_BF16) return MEA_ERR_UNSUPPORTED;
+    if (!table_aligned(s->table, s->table_dtype)) return MEA_ERR_INVALID_ARG;
     if (s->two_sided != 0 && s->two_sided != 1) return MEA_ERR_INVALID_ARG;
     if (!s->edges || s->n_edges < 2 || s->edges[0] != 0) return MEA_ERR_INVALID_ARG;
     if (s->n_edges > MEA_MAX_SIDE_BUCKETS) return MEA_ERR_UNSUPPORTED;
@@ -192,8 +194,8 @@ hipError_t run_combine(const StreamParams& q, const mea_problem* p, int parts, h
 
 mea_status status_of(hipError_t e) { return e == hipSuccess ? MEA_OK : MEA_ERR_HIP; }
 
-// Grids and thread counts that one launch has to hold.
-bool fits_launch(int64_t wgs) { return wgs < ((int64_t)1 << 31) / 256; }
+// Whether one launch holds that many workgroups of 256 threads (2^32 threads).
+bool fits_launch(int64_t wgs) { return wgs < ((int64_t)1 << 24); }
 
 struct BwdWork {
   int64_t n_q_pad, n_qtiles;
@@ -311,7 +313,9 @@ mea_status mea_scored_attention_fwd(const mea_problem* p, const mea_score* s, co
       return MEA_ERR_INVALID_ARG;
   }
   const int64_t grid = w.pl.rtiles * w.pl.groups * w.pl.splits;
-  if (!fits_launch(grid) || !fits_launch((a.out_rows * p->d / 4 + 255) / 256)) return MEA_ERR_INVALID_ARG;
+  if (!fits_launch(grid) || (w.pl.splits > 1 && !fits_launch((a.out_rows * p->d / 4 + 255) / 256)) ||
+      (s->q_doc && !fits_launch(p->batch * ((p->n_k + 31) / 32))))
+    return MEA_ERR_INVALID_ARG;
   if (p->causal)
     a.tile_order = mea::causal_tile_order(p->batch * kv * p->n_k * 2 * p->d * (int64_t)elem_size(p->dtype), grid, true);
   float* at = align256(workspace, 0);
@@ -338,7 +342,7 @@ mea_status mea_scored_attention_bwd(const mea_problem* p, const mea_score* s, co
   if (o_lo && (!aligned16(o_lo) || p->dtype == MEA_F32)) return MEA_ERR_INVALID_ARG;
   if (!aligned16(dq) || !aligned16(dk) || !aligned16(dv) || (dk == nullptr) != (dv == nullptr) || (!dq && !dk))
     return MEA_ERR_INVALID_ARG;
-  if (d_table && (!aligned4(d_table) || !s->table || !dq)) return MEA_ERR_INVALID_ARG;
+  if (d_table && (!s->table || !dq || !table_aligned(d_table, s->table_dtype))) return MEA_ERR_INVALID_ARG;
   const BwdWork w = plan_scored_bwd(p, s);
   if (!workspace || workspace_bytes < w.total) return MEA_ERR_WORKSPACE;
   const int64_t kv = kv_heads_of(p, s->kv_heads);
@@ -380,8 +384,12 @@ mea_status mea_scored_attention_bwd(const mea_problem* p, const mea_score* s, co
         (dk && (!strides_ok(B, kv, a.sdk, p->n_k, true, e, d) || !strides_ok(B, kv, a.sdv, p->n_k, true, e, d))))
       return MEA_ERR_INVALID_ARG;
   }
-  if (!fits_launch(p->batch * p->heads * (w.n_q_pad / 8)) || !fits_launch(p->batch * kv * ((p->n_k + 127) / 128)) ||
-      !fits_launch((p->batch * (p->heads * p->n_q + 2 * kv * p->n_k) + 24) * p->d / 4 / 256))
+  const int64_t rows_wg = 256 / (p->d * (int64_t)elem_size(p->dtype) / 16);
+  const int64_t wgs = p->batch * (kv * w.parts.kv_heads * w.parts.kv_queries * ((p->n_k + 127) / 128) +
+                                  p->heads * w.parts.dq * w.n_qtiles);
+  if (!fits_launch(p->batch * p->heads * w.n_q_pad / rows_wg + 1) || !fits_launch(wgs) ||
+      ((w.kv_sums || w.q_sums) && !fits_launch((p->batch * (p->heads * p->n_q + 2 * kv * p->n_k) + 24) * p->d / 4 / 256)) ||
+      (s->q_doc && !fits_launch(p->batch * ((p->n_k > p->n_q ? p->n_k : p->n_q) + 31) / 32)))
     return MEA_ERR_INVALID_ARG;
   if (p->causal)
     a.tile_order = mea::causal_tile_order(p->batch * kv * p->n_k * 2 * p->d * (int64_t)elem_size(p->dtype), 0, false);

@@ -17,6 +17,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 #include <ATen/ops/empty.h>
 #include <ATen/ops/empty_like.h>
+#include <c10/core/DeviceGuard.h>
 #include <c10/hip/HIPStream.h>
 
 #include <cmath>
@@ -469,6 +470,7 @@ PyObject* ext_scored_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
   mea_status st;
   {
     pybind11::gil_scoped_release no_gil;
+    const c10::DeviceGuard on(q->device());
     const auto opts = at::TensorOptions().dtype(dt).device(q->device());
     size_t bytes = 0;
     st = g_scored_fwd_ws(&p, &s, &bytes);
@@ -535,6 +537,7 @@ PyObject* ext_scored_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
   mea_status st;
   {
     pybind11::gil_scoped_release no_gil;
+    const c10::DeviceGuard on(q->device());
     const auto opts = at::TensorOptions().dtype(dt).device(q->device());
     size_t bytes = 0;
     st = g_scored_bwd_ws(&p, &s, &bytes);
@@ -614,6 +617,7 @@ PyObject* ext_prefix_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
   mea_status st;
   {
     pybind11::gil_scoped_release no_gil;
+    const c10::DeviceGuard on(q->device());
     size_t bytes = 0;
     st = g_prefix_ws(&p, &x, &bytes);
     if (st == MEA_OK) {

@@ -94,7 +94,7 @@ def _int32(name, t, shape, device):
 
 
 def _shapes(q, k, v):
-    if q.dim() != 4 or k.dim() != 4 or v.dim() != 4:
+    if not all(isinstance(t, torch.Tensor) and t.dim() == 4 for t in (q, k, v)):
         raise ValueError("q, k and v must be [B, H, n, d]")
     if q.dtype not in _DTYPE_CODE:
         raise TypeError("unsupported dtype %s" % q.dtype)
@@ -124,15 +124,15 @@ def _score(q, k, causal, softcap, slopes, bias, max_distance, bidirectional, doc
     s = _lib.MeaScore()
     s.kv_heads = k.shape[1]
     if softcap is not None:
-        if not (softcap > 0 and math.isfinite(softcap)):
+        if not (isinstance(softcap, (int, float)) and softcap > 0 and math.isfinite(softcap)):
             raise ValueError("softcap must be positive and finite, got %r" % (softcap,))
         s.softcap = softcap
     if slopes is not None:
-        if slopes.dtype != torch.float32 or slopes.device != q.device or tuple(slopes.shape) != (H,) or not slopes.is_contiguous():
+        if not isinstance(slopes, torch.Tensor) or slopes.dtype != torch.float32 or slopes.device != q.device or tuple(slopes.shape) != (H,) or not slopes.is_contiguous():
             raise ValueError("slopes must be a contiguous float32 [H] tensor on q's device")
         s.slopes = slopes.data_ptr()
     if bias is not None:
-        if bias.dtype not in (torch.float32, q.dtype) or bias.device != q.device or bias.dim() != 2 or bias.shape[1] != H \
+        if not isinstance(bias, torch.Tensor) or bias.dtype not in (torch.float32, q.dtype) or bias.device != q.device or bias.dim() != 2 or bias.shape[1] != H \
                 or not bias.is_contiguous():
             raise ValueError("bias must be a contiguous [buckets, H] tensor on q's device, in float32 or q's dtype")
         two_sided = not causal if bidirectional is None else bool(bidirectional)
@@ -140,6 +140,8 @@ def _score(q, k, causal, softcap, slopes, bias, max_distance, bidirectional, doc
         s.n_edges, s.two_sided = bias.shape[0] // (2 if two_sided else 1), two_sided
         s.table, s.table_dtype = bias.data_ptr(), _DTYPE_CODE[bias.dtype]
     if docs is not None:
+        if not isinstance(docs, torch.Tensor) and len(docs) != 2:
+            raise ValueError("docs must be a tensor, or a pair of those of the queries and of the keys")
         if isinstance(docs, torch.Tensor):
             if n_q != k.shape[2]:
                 raise ValueError("docs must be a pair of [B, n_q] and [B, n_k] tensors where n_q and n_k differ")
@@ -192,9 +194,10 @@ def attention_scored_fwd(q, k, v, causal: bool = False, scale: float | None = No
     o_lo = torch.empty(q.shape, dtype=q.dtype, device=q.device) if residual and q.dtype != torch.float32 else None
     size = _lib.scored_fwd_workspace_size(p, s)
     ws = _workspace(size, q.device)
-    _lib.check("mea_scored_attention_fwd", _lib.scored_fwd(
-        p, s, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), _ptr(lse), _ptr(o_lo), _ptr(ws), size,
-        _stream(q.device)))
+    with torch.cuda.device(q.device):
+        _lib.check("mea_scored_attention_fwd", _lib.scored_fwd(
+            p, s, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), _ptr(lse), _ptr(o_lo), _ptr(ws), size,
+            _stream(q.device)))
     return (o, lse, o_lo) if residual else (o, lse)
 
 
@@ -230,9 +233,10 @@ def attention_scored_bwd(q, k, v, o, lse, do, causal: bool = False, scale: float
     p = _problem(q, k, causal, scale, kv_len, {n: t for n, t in given.items() if t is not None})
     size = _lib.scored_bwd_workspace_size(p, s)
     ws = _workspace(size, q.device)
-    _lib.check("mea_scored_attention_bwd", _lib.scored_bwd(
-        p, s, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), _ptr(o_lo), do.data_ptr(), lse.data_ptr(),
-        _ptr(dq), _ptr(dk), _ptr(dv), _ptr(dbias), _ptr(ws), size, _stream(q.device)))
+    with torch.cuda.device(q.device):
+        _lib.check("mea_scored_attention_bwd", _lib.scored_bwd(
+            p, s, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), _ptr(o_lo), do.data_ptr(), lse.data_ptr(),
+            _ptr(dq), _ptr(dk), _ptr(dv), _ptr(dbias), _ptr(ws), size, _stream(q.device)))
     return dq if need_dq else None, dk, dv, dbias
 
 
@@ -272,6 +276,7 @@ def attention_scored(q, k, v, causal: bool = False, scale: float | None = None, 
     the arguments are those of ``attention_scored_fwd``."""
     if slopes is not None and slopes.requires_grad:
         raise ValueError("slopes get no gradient: pass them detached")
+    docs = tuple(docs) if isinstance(docs, list) else docs
     return ScoredAttention.apply(q, k, v, bias, causal, scale, kv_len, softcap, slopes, max_distance, bidirectional, docs,
                                  prefix_len, q_pos)
 
@@ -309,6 +314,7 @@ def attention_shared_prefix(q, k_prefix, v_prefix, k, v, causal: bool = False, s
     lse = torch.empty(q.shape[:3], dtype=torch.float32, device=q.device) if need_lse else None
     size = _lib.prefix_fwd_workspace_size(p, x)
     ws = _workspace(size, q.device)
-    _lib.check("mea_prefix_attention_fwd", _lib.prefix_fwd(
-        p, x, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), _ptr(lse), _ptr(ws), size, _stream(q.device)))
+    with torch.cuda.device(q.device):
+        _lib.check("mea_prefix_attention_fwd", _lib.prefix_fwd(
+            p, x, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), _ptr(lse), _ptr(ws), size, _stream(q.device)))
     return (o, lse) if need_lse else o
