@@ -14,6 +14,8 @@
 // _lib.check.
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/Exceptions.h>
+#include <torch/csrc/autograd/custom_function.h>
+#include <torch/csrc/autograd/functions/basic_ops.h>
 #include <torch/csrc/autograd/python_variable.h>
 #include <ATen/ops/empty.h>
 #include <ATen/ops/empty_like.h>
@@ -21,7 +23,9 @@
 #include <c10/hip/HIPStream.h>
 
 #include <cmath>
+#include <memory>
 #include <optional>
+#include <vector>
 
 #include "../../include/mea.h"
 
@@ -441,6 +445,71 @@ bool score(mea_score* s, PyObject* const* a, const at::Tensor& q, const at::Tens
   return true;
 }
 
+// The forward into *o (allocated if undefined), *lse and *o_lo as wanted.
+mea_status run_scored_fwd(mea_problem& p, const mea_score& s, const at::Tensor& q, const at::Tensor& k, const at::Tensor& v,
+                          bool need_lse, bool residual, at::Tensor* o, at::Tensor* lse, at::Tensor* o_lo) {
+  const c10::DeviceGuard on(q.device());
+  const auto opts = at::TensorOptions().dtype(q.scalar_type()).device(q.device());
+  size_t bytes = 0;
+  const mea_status st = g_scored_fwd_ws(&p, &s, &bytes);
+  if (st != MEA_OK) return st;
+  if (!o->defined()) *o = at::empty(q.sizes(), opts);
+  mea_strides ms = {};
+  p.strides = nullptr;
+  if (!q.is_contiguous() || !k.is_contiguous() || !v.is_contiguous() || !o->is_contiguous()) {
+    ms.q = strides_of(q);
+    ms.k = strides_of(k);
+    ms.v = strides_of(v);
+    ms.o = strides_of(*o);
+    p.strides = &ms;
+  }
+  if (need_lse) *lse = at::empty(q.sizes().slice(0, 3), opts.dtype(at::kFloat));
+  if (residual && q.scalar_type() != at::kFloat) *o_lo = at::empty(q.sizes(), opts);
+  at::Tensor ws;
+  if (bytes) ws = workspace(bytes, q.device());
+  return g_scored_fwd(&p, &s, q.const_data_ptr(), k.const_data_ptr(), v.const_data_ptr(), o->mutable_data_ptr(),
+                      need_lse ? static_cast<float*>(lse->mutable_data_ptr()) : nullptr,
+                      o_lo->defined() ? o_lo->mutable_data_ptr() : nullptr, bytes ? ws.mutable_data_ptr() : nullptr, bytes,
+                      stream_of(q.device()));
+}
+
+// The backward into g: dq, dk, dv and the bias's gradient, need[] of (dq, dk and dv, the bias's).
+mea_status run_scored_bwd(mea_problem& p, const mea_score& s, const at::Tensor& q, const at::Tensor& k, const at::Tensor& v,
+                          const at::Tensor& o, const at::Tensor& o_lo, const at::Tensor& lse, const at::Tensor& d_o,
+                          const at::Tensor* bias, const int (&need)[3], at::Tensor (&g)[4]) {
+  const c10::DeviceGuard on(q.device());
+  const auto opts = at::TensorOptions().dtype(q.scalar_type()).device(q.device());
+  size_t bytes = 0;
+  mea_status st = g_scored_bwd_ws(&p, &s, &bytes);
+  if (st != MEA_OK) return st;
+  if (need[0] || need[2]) g[0] = at::empty(q.sizes(), opts);
+  if (need[1]) {
+    g[1] = at::empty(k.sizes(), opts);
+    g[2] = at::empty(k.sizes(), opts);
+  }
+  if (need[2]) g[3] = at::empty(bias->sizes(), opts.dtype(bias->scalar_type()));
+  mea_strides ms = {};
+  p.strides = nullptr;
+  if (!q.is_contiguous() || !k.is_contiguous() || !v.is_contiguous() || !o.is_contiguous() || !d_o.is_contiguous()) {
+    ms.q = strides_of(q);
+    ms.k = strides_of(k);
+    ms.v = strides_of(v);
+    ms.o = strides_of(o);
+    ms.d_o = strides_of(d_o);
+    if (g[0].defined()) ms.dq = strides_of(g[0]);
+    if (g[1].defined()) ms.dk = ms.dv = strides_of(g[1]);
+    p.strides = &ms;
+  }
+  at::Tensor ws = workspace(bytes, q.device());
+  auto ptr = [](at::Tensor& t) { return t.defined() ? t.mutable_data_ptr() : nullptr; };
+  st = g_scored_bwd(&p, &s, q.const_data_ptr(), k.const_data_ptr(), v.const_data_ptr(), o.const_data_ptr(),
+                    o_lo.defined() ? o_lo.const_data_ptr() : nullptr, d_o.const_data_ptr(),
+                    static_cast<const float*>(lse.const_data_ptr()), ptr(g[0]), ptr(g[1]), ptr(g[2]), ptr(g[3]),
+                    ws.mutable_data_ptr(), bytes, stream_of(q.device()));
+  if (!need[0]) g[0] = at::Tensor();
+  return st;
+}
+
 // scored_fwd(q, k, v, causal, scale, need_lse, out, kv_len, residual, <score>):
 // attention_scored_fwd's result, or None.
 PyObject* ext_scored_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
@@ -467,32 +536,11 @@ PyObject* ext_scored_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return none();
   }
   at::Tensor o, lse, o_lo;
+  if (out) o = *out;
   mea_status st;
   {
     pybind11::gil_scoped_release no_gil;
-    const c10::DeviceGuard on(q->device());
-    const auto opts = at::TensorOptions().dtype(dt).device(q->device());
-    size_t bytes = 0;
-    st = g_scored_fwd_ws(&p, &s, &bytes);
-    if (st == MEA_OK) {
-      o = out ? *out : at::empty(q->sizes(), opts);
-      mea_strides ms = {};
-      if (!q->is_contiguous() || !k->is_contiguous() || !v->is_contiguous() || !o.is_contiguous()) {
-        ms.q = strides_of(*q);
-        ms.k = strides_of(*k);
-        ms.v = strides_of(*v);
-        ms.o = strides_of(o);
-        p.strides = &ms;
-      }
-      if (need_lse) lse = at::empty(q->sizes().slice(0, 3), at::TensorOptions().dtype(at::kFloat).device(q->device()));
-      if (residual && dt != at::kFloat) o_lo = at::empty(q->sizes(), opts);
-      at::Tensor ws;
-      if (bytes) ws = workspace(bytes, q->device());
-      st = g_scored_fwd(&p, &s, q->const_data_ptr(), k->const_data_ptr(), v->const_data_ptr(), o.mutable_data_ptr(),
-                        lse.defined() ? static_cast<float*>(lse.mutable_data_ptr()) : nullptr,
-                        o_lo.defined() ? o_lo.mutable_data_ptr() : nullptr, bytes ? ws.mutable_data_ptr() : nullptr, bytes,
-                        stream_of(q->device()));
-    }
+    st = run_scored_fwd(p, s, *q, *k, *v, need_lse, residual, &o, &lse, &o_lo);
   }
   if (st != MEA_OK) return failed("mea_scored_attention_fwd", st);
   return residual ? tuple_of({o, lse, o_lo}) : tuple_of({o, lse});
@@ -533,43 +581,137 @@ PyObject* ext_scored_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
   }
   if (!bias) need[2] = 0;
   if (!(need[0] || need[1] || need[2])) return none();
-  at::Tensor dq, dk, dv, db;
+  at::Tensor g[4];
   mea_status st;
   {
     pybind11::gil_scoped_release no_gil;
-    const c10::DeviceGuard on(q->device());
-    const auto opts = at::TensorOptions().dtype(dt).device(q->device());
-    size_t bytes = 0;
-    st = g_scored_bwd_ws(&p, &s, &bytes);
-    if (st == MEA_OK) {
-      if (need[0] || need[2]) dq = at::empty(q->sizes(), opts);
-      if (need[1]) {
-        dk = at::empty(k->sizes(), opts);
-        dv = at::empty(k->sizes(), opts);
-      }
-      if (need[2]) db = at::empty(bias->sizes(), opts.dtype(bias->scalar_type()));
-      mea_strides ms = {};
-      if (!q->is_contiguous() || !k->is_contiguous() || !v->is_contiguous() || !o->is_contiguous() || !d_o->is_contiguous()) {
-        ms.q = strides_of(*q);
-        ms.k = strides_of(*k);
-        ms.v = strides_of(*v);
-        ms.o = strides_of(*o);
-        ms.d_o = strides_of(*d_o);
-        if (dq.defined()) ms.dq = strides_of(dq);
-        if (dk.defined()) ms.dk = ms.dv = strides_of(dk);
-        p.strides = &ms;
-      }
-      at::Tensor ws = workspace(bytes, q->device());
-      auto ptr = [](at::Tensor& t) { return t.defined() ? t.mutable_data_ptr() : nullptr; };
-      st = g_scored_bwd(&p, &s, q->const_data_ptr(), k->const_data_ptr(), v->const_data_ptr(), o->const_data_ptr(),
-                        o_lo ? o_lo->const_data_ptr() : nullptr, d_o->const_data_ptr(),
-                        static_cast<const float*>(lse->const_data_ptr()), ptr(dq), ptr(dk), ptr(dv), ptr(db),
-                        ws.mutable_data_ptr(), bytes, stream_of(q->device()));
-    }
+    st = run_scored_bwd(p, s, *q, *k, *v, *o, o_lo ? *o_lo : at::Tensor(), *lse, *d_o, bias, need, g);
   }
   if (st != MEA_OK) return failed("mea_scored_attention_bwd", st);
-  if (!need[0]) dq = at::Tensor();
-  return tuple_of({dq, dk, dv, db});
+  return tuple_of({g[0], g[1], g[2], g[3]});
+  END_HANDLE_TH_ERRORS
+}
+
+// The differentiable call without Python in it: a backward that autograd's thread runs
+// on its own (a training step on a small problem is bound by the host, and by the
+// hand-over of the interpreter between the two threads).
+struct Refused {
+  mea_status st;
+};
+struct ScoredNode : public torch::autograd::Function<ScoredNode> {
+  // extra: kv_len, slopes, q_doc, k_doc, prefix_len, q_pos, where given.
+  static at::Tensor forward(torch::autograd::AutogradContext* ctx, at::Tensor q, at::Tensor k, at::Tensor v,
+                            std::optional<at::Tensor> bias, mea_problem p, mea_score s, std::vector<at::Tensor> extra) {
+    at::Tensor o, lse, o_lo;
+    const mea_status st = run_scored_fwd(p, s, q, k, v, true, true, &o, &lse, &o_lo);
+    if (st != MEA_OK) throw Refused{st};
+    torch::autograd::variable_list saved = {q, k, v, bias ? *bias : at::Tensor(), o, lse, o_lo};
+    for (const at::Tensor& t : extra) saved.push_back(t);
+    ctx->save_for_backward(std::move(saved));
+    ctx->saved_data["i"] = std::vector<int64_t>{p.causal, (int64_t)reinterpret_cast<uintptr_t>(s.edges), s.n_edges, s.two_sided};
+    ctx->saved_data["f"] = std::vector<double>{p.scale, s.softcap};
+    return o;
+  }
+  static torch::autograd::variable_list backward(torch::autograd::AutogradContext* ctx, torch::autograd::variable_list grads) {
+    torch::autograd::variable_list none(7);
+    if (!grads[0].defined()) return none;
+    const auto t = ctx->get_saved_variables();
+    const at::Tensor &q = t[0], &k = t[1], &v = t[2], &bias = t[3], &o = t[4], &lse = t[5], &o_lo = t[6];
+    at::Tensor g[4];
+    mea_status st;
+    {
+      const at::AutoGradMode no_grad(false);
+      at::Tensor d_o = grads[0];
+      if (d_o.scalar_type() != q.scalar_type()) d_o = d_o.to(q.scalar_type());
+      if (!in_place(d_o)) d_o = d_o.contiguous();
+      const auto i = ctx->saved_data["i"].toIntVector();
+      const auto f = ctx->saved_data["f"].toDoubleVector();
+      auto ptr = [&](int at) { return t[at].defined() ? t[at].const_data_ptr() : nullptr; };
+      mea_problem p = {};
+      p.batch = q.size(0);
+      p.heads = q.size(1);
+      p.n_q = q.size(2);
+      p.n_k = k.size(2);
+      p.d = q.size(3);
+      p.dtype = dtype_code(q.scalar_type());
+      p.causal = (int32_t)i[0];
+      p.scale = (float)f[0];
+      p.kv_len = static_cast<const int32_t*>(ptr(7));
+      mea_score s = {};
+      s.kv_heads = k.size(1);
+      s.softcap = (float)f[1];
+      s.edges = reinterpret_cast<const int32_t*>((uintptr_t)i[1]);
+      s.n_edges = (int32_t)i[2];
+      s.two_sided = (int32_t)i[3];
+      if (bias.defined()) {
+        s.table = bias.const_data_ptr();
+        s.table_dtype = dtype_code(bias.scalar_type());
+      }
+      s.slopes = static_cast<const float*>(ptr(8));
+      s.q_doc = static_cast<const int32_t*>(ptr(9));
+      s.k_doc = static_cast<const int32_t*>(ptr(10));
+      s.prefix_len = static_cast<const int32_t*>(ptr(11));
+      s.q_pos = static_cast<const int32_t*>(ptr(12));
+      const int need[3] = {ctx->needs_input_grad(0), ctx->needs_input_grad(1) || ctx->needs_input_grad(2),
+                           bias.defined() && ctx->needs_input_grad(3)};
+      if (!(need[0] || need[1] || need[2])) return none;
+      st = run_scored_bwd(p, s, q, k, v, o, o_lo, lse, d_o, &bias, need, g);
+    }
+    if (st != MEA_OK) {
+      pybind11::gil_scoped_acquire gil;
+      Py_XDECREF(PyObject_CallFunction(g_check, "si", "mea_scored_attention_bwd", (int)st));
+      python_error e;
+      e.persist();
+      throw e;
+    }
+    torch::autograd::variable_list r = {g[0], g[1], g[2], g[3]};
+    if (at::GradMode::is_enabled()) {  // create_graph: the gradient cannot be differentiated again
+      auto error = std::make_shared<torch::autograd::DelayedError>("scored attention cannot be differentiated twice", 4);
+      r = (*error)(std::move(r));
+    }
+    r.resize(7);
+    return r;
+  }
+};
+
+// scored_apply(q, k, v, causal, scale, kv_len, <score>): o, with its gradient, or None.
+PyObject* ext_scored_apply(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  if (n != 14) return none();
+  const at::Tensor *q = gpu_tensor(a[0]), *k = gpu_tensor(a[1]), *v = gpu_tensor(a[2]), *bias;
+  if (!q || !k || !v) return none();
+  const at::ScalarType dt = q->scalar_type();
+  if (dtype_code(dt) < 0 || !in_place(*q) || !like(*k, *q, dt) || !like(*v, *q, dt) || !grouped_shapes(*q, *k, *v))
+    return none();
+  mea_problem p;
+  mea_score s;
+  if (!problem(&p, q->size(0), q->size(1), q->size(2), k->size(2), q->size(3), q->size(3), dtype_code(dt), a[3], a[4], a[5],
+               q->device(), false) ||
+      !score(&s, a + 6, *q, *k, &bias)) {
+    PyErr_Clear();
+    return none();
+  }
+  const bool grad = at::GradMode::is_enabled() &&
+                    (q->requires_grad() || k->requires_grad() || v->requires_grad() || (bias && bias->requires_grad()));
+  // (checked above: a tensor or None)
+  std::vector<at::Tensor> extra;
+  for (PyObject* o : {a[5], a[7], a[10], a[11], a[12], a[13]}) extra.push_back(o == Py_None ? at::Tensor() : *gpu_tensor(o));
+  at::Tensor o, lse, o_lo;
+  mea_status st = MEA_OK;
+  {
+    pybind11::gil_scoped_release no_gil;
+    if (grad) {
+      try {
+        o = ScoredNode::apply(*q, *k, *v, bias ? std::optional<at::Tensor>(*bias) : std::nullopt, p, s, std::move(extra));
+      } catch (const Refused& r) {
+        st = r.st;
+      }
+    } else {
+      st = run_scored_fwd(p, s, *q, *k, *v, false, false, &o, &lse, &o_lo);
+    }
+  }
+  if (st != MEA_OK) return failed("mea_scored_attention_fwd", st);
+  return THPVariable_Wrap(o);
   END_HANDLE_TH_ERRORS
 }
 
@@ -697,6 +839,7 @@ PyMethodDef methods[] = {
     {"init_scored", fast(ext_init_scored), METH_FASTCALL, nullptr},
     {"scored_fwd", fast(ext_scored_fwd), METH_FASTCALL, nullptr},
     {"scored_bwd", fast(ext_scored_bwd), METH_FASTCALL, nullptr},
+    {"scored_apply", fast(ext_scored_apply), METH_FASTCALL, nullptr},
     {"prefix_fwd", fast(ext_prefix_fwd), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };

@@ -241,7 +241,8 @@ def attention_scored_bwd(q, k, v, o, lse, do, causal: bool = False, scale: float
 
 
 class ScoredAttention(torch.autograd.Function):
-    """Autograd wrapper: saves q, k, v, o, the O(n) lse and, for a 16-bit o, its rounding residual."""
+    """Autograd wrapper of what the native call leaves (copies to readable layouts, errors): saves
+    q, k, v, o, the O(n) lse and, for a 16-bit o, its rounding residual."""
 
     @staticmethod
     def forward(ctx, q, k, v, bias, causal, scale, kv_len, softcap, slopes, max_distance, bidirectional, docs, prefix_len,
@@ -277,6 +278,11 @@ def attention_scored(q, k, v, causal: bool = False, scale: float | None = None, 
     if slopes is not None and slopes.requires_grad:
         raise ValueError("slopes get no gradient: pass them detached")
     docs = tuple(docs) if isinstance(docs, list) else docs
+    mods = _native_score(causal, softcap, slopes, bias, max_distance, bidirectional, docs, prefix_len, q_pos)
+    if mods is not None:
+        r = _lib.native().scored_apply(q, k, v, causal, scale, kv_len, *mods)
+        if r is not None:
+            return r
     return ScoredAttention.apply(q, k, v, bias, causal, scale, kv_len, softcap, slopes, max_distance, bidirectional, docs,
                                  prefix_len, q_pos)
 

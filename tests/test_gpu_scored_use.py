@@ -174,7 +174,7 @@ def test_streams():
 class _Off:
     """Native calls that accept nothing."""
 
-    scored_fwd = scored_bwd = prefix_fwd = staticmethod(lambda *a: None)
+    scored_fwd = scored_bwd = scored_apply = prefix_fwd = staticmethod(lambda *a: None)
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
