@@ -251,6 +251,12 @@ __device__ __forceinline__ float cap_tanh(const ScoreArgs& s, float x) {
   return t;
 }
 
+// A value that the compiler takes as made here, so that what depends on it stays in
+// this branch: as selects on the branch's condition, the masks of a few tiles cost every
+// tile two instructions an element (an empty volatile statement did not prevent it).
+__device__ __forceinline__ void stay(int& x) { asm volatile("" : "+v"(x)); }
+__device__ __forceinline__ void stay(float& x) { asm volatile("" : "+v"(x)); }
+
 // Keys visible to a query by position: [0, lim).  reach: keys that every query sees
 // (a prefix; all of them without the causal mask).
 __device__ __forceinline__ int64_t key_limit(int64_t n_kv, int64_t reach, int64_t pos) {

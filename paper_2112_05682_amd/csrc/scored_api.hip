@@ -109,7 +109,7 @@ void set_tiles(StreamPlan* pl, const mea_problem* p, int rw, int64_t n_keys, int
   pl->splits = splits < 1 ? 1 : splits;
 }
 
-// Fold: with few queries the heads that share a key head are rows of the same
+// Fold: with few queries (a 32-row tile of one head would be padding) the heads that share a key head are rows of the same
 // tile, so that the keys are read once for all of them; with many, each head has
 // tiles of its own (the keys are then found in L2).  Row waves: as few as hold
 // the rows, and on small grids fewer still, so that the waves without rows of
@@ -119,7 +119,7 @@ StreamPlan plan_stream(const mea_problem* p, const ScoreArgs& s, int64_t kv_head
   StreamPlan pl;
   const bool is16 = p->dtype != MEA_F32;
   const int64_t G = p->heads / kv_heads;
-  pl.fold = G * p->n_q <= 64 ? G : 1;
+  pl.fold = p->n_q <= 32 || G * p->n_q <= 64 ? G : 1;
   // The biases of the folded heads have to fit beside the stages.
   if (pl.fold > 1 && mea::bias_lds_bytes(s, (int)pl.fold) > 24 * 1024) pl.fold = 1;
   pl.rows = p->n_q * pl.fold;

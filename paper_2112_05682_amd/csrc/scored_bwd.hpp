@@ -306,8 +306,8 @@ __device__ __forceinline__ void dkdv_workgroup(const ScoredBwdParams& p, int blo
 #pragma unroll
             for (int r = 0; r < 16; ++r) s[r] = fmaf((float)permuted_row(r, 0), -slope, s[r]);
           } else {
-            asm volatile("");
-            const float d0 = (float)off;
+            float d0 = (float)off;
+            stay(d0);
 #pragma unroll
             for (int r = 0; r < 16; ++r) s[r] = fmaf(-fabsf(d0 - (float)permuted_row(r, 0)), slope, s[r]);
           }
@@ -317,22 +317,22 @@ __device__ __forceinline__ void dkdv_workgroup(const ScoredBwdParams& p, int blo
           if (kw + 31 <= p_lo - sa.span || kw >= p_hi + hi) {
             add += reinterpret_cast<const float*>(lds_bias)[kw >= p_hi + hi ? bias_places(sa) - 1 : 0];
           } else {
-            asm volatile("");
-            const float* at = reinterpret_cast<const float*>(lds_bias) + (off + sa.span + kPad);
+            int from = off + sa.span + kPad;
+            stay(from);
+            const float* at = reinterpret_cast<const float*>(lds_bias) + from;
 #pragma unroll
             for (int r = 0; r < 16; ++r) s[r] += at[-permuted_row(r, 0)];
           }
         }
       }
       if (masked) {
-        asm volatile("");
-        const int m = min_q - (int)q0 - 8 * h;
+        int m = min_q - (int)q0 - 8 * h;
+        stay(m);
 #pragma unroll
         for (int r = 0; r < 16; ++r)
           if (permuted_row(r, 0) < m) s[r] = -INFINITY;
       }
       if (by_doc) {
-        asm volatile("");
         const int mine = q0 + c < p.n_q ? sa.q_doc[(int64_t)b * p.n_q + q0 + c] : -1;
         hide_documents(s, doc, mine, tile_ids[wave], lane);
       }
@@ -714,8 +714,8 @@ __device__ __forceinline__ void dq_workgroup(const ScoredBwdParams& p, int block
 #pragma unroll
             for (int r = 0; r < 16; ++r) s[r] = fmaf((float)permuted_row(r, 0), slope, s[r]);
           } else {
-            asm volatile("");
-            const float d0 = (float)off;
+            float d0 = (float)off;
+            stay(d0);
 #pragma unroll
             for (int r = 0; r < 16; ++r) s[r] = fmaf(-fabsf(d0 + (float)permuted_row(r, 0)), slope, s[r]);
           }
@@ -724,22 +724,22 @@ __device__ __forceinline__ void dq_workgroup(const ScoredBwdParams& p, int block
           if (far) {
             add += reinterpret_cast<const float*>(lds_bias)[k0 >= p_hi + hi ? places - 1 : 0];
           } else {
-            asm volatile("");
-            const float* at = reinterpret_cast<const float*>(lds_bias) + (off + sa.span + kPad);
+            int from = off + sa.span + kPad;
+            stay(from);
+            const float* at = reinterpret_cast<const float*>(lds_bias) + from;
 #pragma unroll
             for (int r = 0; r < 16; ++r) s[r] += at[permuted_row(r, 0)];
           }
         }
       }
       if (masked) {
-        asm volatile("");
-        const int m = lim - (int)k0 - 8 * h;
+        int m = lim - (int)k0 - 8 * h;
+        stay(m);
 #pragma unroll
         for (int r = 0; r < 16; ++r)
           if (permuted_row(r, 0) >= m) s[r] = -INFINITY;
       }
       if (by_doc) {
-        asm volatile("");
         const int mine = k0 + c < p.n_k ? sa.k_doc[(int64_t)b * p.n_k + k0 + c] : -1;
         hide_documents(s, doc, mine, tile_ids[wave], lane);
       }
@@ -756,7 +756,6 @@ __device__ __forceinline__ void dq_workgroup(const ScoredBwdParams& p, int block
             if (k0 >= p_hi + hi) far_hi += x;
             else far_lo += x;
           } else {
-            asm volatile("");
             // A lane adds a diagonal of the wave's tile.  (LDS atomics by distance took 166
             // cycles an instruction; this takes 48 reads and writes for 16 of them.)
             float* const to = skew + 63 * c + 31 + 8 * h;

@@ -194,9 +194,8 @@ __device__ __forceinline__ void stream_workgroup(const StreamParams& p, int bloc
   const int krow = perm32(c);
 
   // One tile: masked, some key is beyond some row's limit; by_doc, documents differ.
-  // The masks are uniform branches (an empty volatile statement each, so that they do
-  // not become selects in every tile) of one copy of the code: with a copy each for
-  // plain and masked tiles the d = 64 kernels spilled 84-173 registers in the loop.
+  // The masks are uniform branches of one copy of the code: with a copy each for plain
+  // and masked tiles the d = 64 kernels spilled 84-173 registers in the loop.
   auto tile = [&](int t, int buf, bool masked, bool by_doc) __attribute__((always_inline)) {
     const int64_t k0 = (int64_t)t * BK + BKW * wave_k;
     if (k0 >= w_lim) return;  // all keys beyond this wave's rows
@@ -246,8 +245,8 @@ __device__ __forceinline__ void stream_workgroup(const StreamParams& p, int bloc
 #pragma unroll
             for (int r = 0; r < 16; ++r) s[kt][r] = fmaf((float)(32 * kt + permuted_row(r, 0)), slope, s[kt][r]);
         } else {
-          asm volatile("");
-          const float d0 = (float)off;
+          float d0 = (float)off;
+          stay(d0);
 #pragma unroll
           for (int kt = 0; kt < NKT; ++kt)
 #pragma unroll
@@ -259,7 +258,8 @@ __device__ __forceinline__ void stream_workgroup(const StreamParams& p, int bloc
         if (k0 + BKW - 1 <= wq_lo - sa.span || k0 >= wq_hi + hi) {  // one value for every key of a row
           add += bias_at(sa, lds_bias, p.fold, (int)g, k0 >= wq_hi + hi ? last : 0);
         } else {
-          asm volatile("");
+          int at_off = off;
+          stay(at_off);
 #pragma unroll
           for (int kt = 0; kt < NKT; ++kt) {
             const int64_t ka = k0 + 32 * kt;
@@ -268,13 +268,13 @@ __device__ __forceinline__ void stream_workgroup(const StreamParams& p, int bloc
 #pragma unroll
               for (int r = 0; r < 16; ++r) s[kt][r] += v;
             } else if (p.fold == 1) {
-              const float* at = reinterpret_cast<const float*>(lds_bias) + (off + 32 * kt + sa.span + kPad);
+              const float* at = reinterpret_cast<const float*>(lds_bias) + (at_off + 32 * kt + sa.span + kPad);
 #pragma unroll
               for (int r = 0; r < 16; ++r) s[kt][r] += at[permuted_row(r, 0)];
             } else {
 #pragma unroll
               for (int r = 0; r < 16; ++r)
-                s[kt][r] += bias_at(sa, lds_bias, p.fold, (int)g, off + 32 * kt + permuted_row(r, 0) + sa.span + kPad);
+                s[kt][r] += bias_at(sa, lds_bias, p.fold, (int)g, at_off + 32 * kt + permuted_row(r, 0) + sa.span + kPad);
             }
           }
         }
@@ -283,8 +283,8 @@ __device__ __forceinline__ void stream_workgroup(const StreamParams& p, int bloc
 
     // Masks.
     if (masked) {
-      asm volatile("");
-      const int l = lim - (int)k0 - 8 * h;
+      int l = lim - (int)k0 - 8 * h;
+      stay(l);
 #pragma unroll
       for (int kt = 0; kt < NKT; ++kt)
 #pragma unroll
@@ -292,7 +292,6 @@ __device__ __forceinline__ void stream_workgroup(const StreamParams& p, int bloc
           if (32 * kt + permuted_row(r, 0) >= l) s[kt][r] = -INFINITY;
     }
     if (by_doc) {
-      asm volatile("");
 #pragma unroll
       for (int kt = 0; kt < NKT; ++kt) {
         const int64_t key = k0 + 32 * kt + c;

@@ -110,6 +110,7 @@ DECODE = [  # dtype, B, H, Hkv, nq, nk, d, kv_len
     ("bf16", 2, 8, 2, 1, 3000, 128, [3000, 1]), ("fp16", 3, 4, 4, 3, 1500, 64, [1500, 700, 3]),
     ("fp32", 2, 6, 2, 1, 900, 64, [900, 33]), ("bf16", 1, 12, 1, 5, 777, 64, [777]), ("bf16", 2, 3, 1, 16, 260, 128, [260, 16]),
     ("fp32", 2, 4, 4, 2, 2100, 128, [2100, 2]), ("bf16", 1, 1, 1, 1, 1, 64, [1]), ("fp16", 2, 40, 1, 1, 400, 128, [400, 399]),
+    ("bf16", 1, 130, 1, 1, 500, 64, [500]), ("fp32", 1, 71, 1, 3, 150, 64, [150]), ("fp16", 2, 24, 2, 30, 333, 64, [333, 40]),
 ]
 
 
