@@ -249,15 +249,28 @@ PrefixWork plan_prefix(const mea_problem* p, const mea_shared_prefix* x) {
   // Four row waves read the prefix a quarter as often as one does, which pays on large
   // ones; short or few rows rather share the keys of a tile.  us, row waves 1 / 4, at the
   // best number of ranges each, bf16 d = 128: 256 rows of 8 key heads on 16384 keys 73 / 64,
-  // 800 of 8 on 30000 281 / 164, 864 of 3 on 1329 30 / 32, 64 of 8 on 8192 30 / 31; d = 64: 512
+  // 800 of 8 on 30000 281 / 134, 864 of 3 on 1329 30 / 32, 64 of 8 on 8192 30 / 31; d = 64: 512
   // of 4 on 4000 24 / 27.
   const bool large = w.shared.rows > 64 && (double)(kv * w.shared.rows) * (double)x->n_p > 16e6;
   const int own_least = w.own.rows <= 64 ? 2 : 4;
   const int rwa = large || w.own.rows > 64 ? 4 : (is16 && w.own.rows <= 32 ? 1 : (is16 ? 4 : 2));
   const int rwb = rwa == 4 ? own_least : rwa;
   set_tiles(&w.own, p, rwb, p->n_k, 0);
+  // Ranges of the own keys have 4 tiles and more: in shorter ones the parts cost more than
+  // they spare (27 sequences of 650, d = 128: 19 us in one range, 26 in more).
+  const int64_t long_tiles = p->n_k / (4 * mea::stream_tile(is16, rwb));
+  if (w.own.splits > long_tiles) w.own.splits = long_tiles;
   if (w.own.splits > 8) w.own.splits = 8;
-  set_tiles(&w.shared, p, rwa, x->n_p, w.own.groups * w.own.rtiles * w.own.splits);
+  if (w.own.splits < 1) w.own.splits = 1;
+  // The own keys' workgroups take places from the prefix: as many as they are, of a large
+  // prefix their share of the work (800 rows of 8 on 30000: 134 us, 172 the other way).
+  int64_t taken = w.own.groups * w.own.rtiles * w.own.splits;
+  if (large) {
+    const double own = (double)(w.own.groups * w.own.rtiles * 32 * rwb) * (double)p->n_k;
+    const double pre = (double)(w.shared.groups * ((w.shared.rows + 127) / 128 * 128)) * (double)x->n_p;
+    taken = (int64_t)(own / (own + pre) * (double)places_of(p, rwa));
+  }
+  set_tiles(&w.shared, p, rwa, x->n_p, taken);
   w.total = part_bytes(p, w.shared.splits + w.own.splits) + 256;
   return w;
 }
