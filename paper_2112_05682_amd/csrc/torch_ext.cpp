@@ -730,7 +730,8 @@ PyObject* ext_prefix_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
   for (const at::Tensor* t : {kp, vp})
     if (t->device() != q->device() || t->scalar_type() != dt || t->dim() != 3 || t->stride(2) != 1 ||
         reinterpret_cast<uintptr_t>(t->const_data_ptr()) % 16 || t->stride(0) % unit || t->stride(1) % unit ||
-        t->size(0) != k->size(1) || t->size(2) != q->size(3) || t->size(1) != kp->size(1))
+        t->size(0) != k->size(1) || t->size(2) != q->size(3) || t->size(1) != kp->size(1) ||
+        t->stride(1) < t->size(2))  // (a row stride of 0 would be read as contiguous)
       return none();
   const at::Tensor* out = nullptr;
   if (a[9] != Py_None) {

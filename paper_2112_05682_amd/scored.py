@@ -287,6 +287,14 @@ def attention_scored(q, k, v, causal: bool = False, scale: float | None = None, 
                                  prefix_len, q_pos)
 
 
+def _prefix_strides(name, t):
+    """Head and row strides of a ``[H_kv, n_p, d]`` prefix (of one row: any valid row stride)."""
+    head, row = (s if size > 1 else t.shape[2] for s, size in zip(t.stride()[:2], t.shape[:2]))
+    if row < t.shape[2]:  # (the ABI reads a row stride of 0 as contiguous)
+        raise ValueError("the rows of %s overlap: strides %s" % (name, t.stride()))
+    return _lib.MeaTensorStrides(0, head, row)
+
+
 def attention_shared_prefix(q, k_prefix, v_prefix, k, v, causal: bool = False, scale: float | None = None, kv_len=None, *,
                             q_pos=None, out=None, need_lse: bool = False):
     """Attention of a batch whose sequences begin with the same keys: every query sees all of
@@ -312,9 +320,7 @@ def attention_shared_prefix(q, k_prefix, v_prefix, k, v, causal: bool = False, s
     p = _problem(q, k, causal, scale, kv_len, {"q": q, "k": k, "v": v, "o": o})
     x = _lib.MeaSharedPrefix()
     x.kv_heads, x.n_p, x.k, x.v = k.shape[1], kp.shape[2], kp.data_ptr(), vp.data_ptr()
-    for name, t in (("k_strides", kp), ("v_strides", vp)):
-        h, r = (s if size > 1 else t.shape[3] for s, size in zip(t.stride()[1:3], t.shape[1:3]))
-        setattr(x, name, _lib.MeaTensorStrides(0, h, r))
+    x.k_strides, x.v_strides = _prefix_strides("k_prefix", k_prefix), _prefix_strides("v_prefix", v_prefix)
     if q_pos is not None:
         x.q_pos = _int32("q_pos", q_pos, (q.shape[0],), q.device).data_ptr()
     lse = torch.empty(q.shape[:3], dtype=torch.float32, device=q.device) if need_lse else None

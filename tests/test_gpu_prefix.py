@@ -74,3 +74,19 @@ def test_strides(dtype):
     assert attention_shared_prefix(dev[0], kg, vg, dev[1], dev[2], out=out) is out
     torch.cuda.synchronize()
     assert_within("o", out, ref["o"])
+
+
+def test_broadcast_prefix():
+    """One key that all heads share (both strides 0), and rows that overlap, which are refused."""
+    case = ("bf16", 2, 4, 4, 1, 1, 9, 64, False, None)
+    q, kp, vp, k, v = make(case)
+    kp, vp = kp[:1, 0].expand(4, 1, 64), vp[:1, 0].expand(4, 1, 64)
+    ref = expected(case, q, kp.contiguous(), vp.contiguous(), k, v)
+    dev = [t.cuda() for t in (q, k, v)]
+    kg, vg = (t[0, 0].cuda().as_strided((4, 1, 64), (0, 0, 1)) for t in (kp, vp))
+    o = attention_shared_prefix(dev[0], kg, vg, dev[1], dev[2])
+    torch.cuda.synchronize()
+    assert_within("o", o, ref["o"])
+    long = kg.expand(4, 30, 64)
+    with pytest.raises(ValueError, match="overlap"):
+        attention_shared_prefix(dev[0], long, long, dev[1], dev[2])

@@ -218,3 +218,16 @@ def test_host_code_under_address_and_undefined_sanitizers(tmp_path):
         assert r.returncode == 0, "%s\n%s\n%s" % (" ".join(cmd), r.stdout[-2000:], r.stderr[-3000:])
     assert "scored_check ok" in r.stdout
     print(r.stdout)
+
+
+def test_strides_of_a_prefix():
+    """A row stride of 0 would mean contiguous rows to the library."""
+    from paper_2112_05682_amd.scored import _prefix_strides
+    one = torch.zeros(64).expand(3, 1, 64)  # one key for all heads
+    s = _prefix_strides("k_prefix", one)
+    assert (s.head, s.row) == (0, 64)
+    s = _prefix_strides("k_prefix", torch.zeros(5, 3, 64).transpose(0, 1))
+    assert (s.head, s.row) == (64, 192)
+    for t in (torch.zeros(3, 1, 64).expand(3, 7, 64), torch.zeros(500).as_strided((3, 4, 64), (64, 32, 1))):
+        with pytest.raises(ValueError, match="overlap"):
+            _prefix_strides("k_prefix", t)
