@@ -464,6 +464,12 @@ template <typename T> hipError_t launch_stream(const StreamParams& p, int d, int
 // Two key sets in one launch: row waves 4 and 4 or 2, or 1 and 1 (float32: 2 and 2).
 template <typename T>
 hipError_t launch_stream_pair(const StreamParams& a, const StreamParams& b, int d, int rwa, int rwb, hipStream_t stream);
+// Threads that share a row's ranges in the combine, and its workgroups.
+constexpr int kCombineShares = 8;
+inline int combine_shares(int64_t n_parts) { return n_parts > 8 ? kCombineShares : 1; }
+inline int64_t combine_blocks(int64_t rows, int64_t d, int64_t n_parts) {
+  return (rows * (d / 4) * combine_shares(n_parts) + 255) / 256;
+}
 template <typename T>
 hipError_t launch_scored_combine(const StreamParams& p, int d, int n_parts, hipStream_t stream);
 template <typename T> hipError_t launch_scored_bwd(const ScoredBwdParams& p, int d, hipStream_t stream);

@@ -97,7 +97,9 @@ int64_t places_of(const mea_problem* p, int row_waves) {
   if (p->dtype == MEA_F32) return 256;
   return 256 * (row_waves == 1 && p->d == 128 ? 1 : 2);
 }
-// Row tiles, and key ranges for the places that `taken` workgroups leave.
+// Row tiles, and key ranges for the places that `taken` workgroups leave.  At most 256
+// ranges; us at 64 / 128 / 256 of them, one token, 8 heads of one key head: bf16 d = 128
+// 131072 keys 30 / 23 / 22, d = 64 65536 keys 18 / 15 / 15, float32 65536 keys 85 / 50 / 36.
 void set_tiles(StreamPlan* pl, const mea_problem* p, int rw, int64_t n_keys, int64_t taken) {
   pl->row_waves = rw;
   pl->rtiles = (pl->rows + 32 * rw - 1) / (32 * rw);
@@ -105,7 +107,7 @@ void set_tiles(StreamPlan* pl, const mea_problem* p, int rw, int64_t n_keys, int
   const int64_t key_tiles = (n_keys + tile - 1) / tile, places = places_of(p, rw);
   int64_t splits = (places - (taken < places / 2 ? taken : places / 2)) / wgs;
   if (splits > key_tiles / 2) splits = key_tiles / 2;
-  if (splits > 64) splits = 64;
+  if (splits > 256) splits = 256;
   pl->splits = splits < 1 ? 1 : splits;
 }
 
@@ -326,7 +328,7 @@ mea_status mea_scored_attention_fwd(const mea_problem* p, const mea_score* s, co
       return MEA_ERR_INVALID_ARG;
   }
   const int64_t grid = w.pl.rtiles * w.pl.groups * w.pl.splits;
-  if (!fits_launch(grid) || (w.pl.splits > 1 && !fits_launch((a.out_rows * p->d / 4 + 255) / 256)) ||
+  if (!fits_launch(grid) || (w.pl.splits > 1 && !fits_launch(mea::combine_blocks(a.out_rows, p->d, w.pl.splits))) ||
       (s->q_doc && !fits_launch(p->batch * ((p->n_k + 31) / 32))))
     return MEA_ERR_INVALID_ARG;
   if (p->causal)
@@ -479,10 +481,10 @@ mea_status mea_prefix_attention_fwd(const mea_problem* p, const mea_shared_prefi
       !strides_ok(p->batch, kv, own.sv, p->n_k, false, e, d) || !strides_ok(p->batch, p->heads, own.so, p->n_q, true, e, d) ||
       !strides_ok(1, kv, spk, x->n_p, false, e, d) || !strides_ok(1, kv, spv, x->n_p, false, e, d))
     return MEA_ERR_INVALID_ARG;
-  if (!fits_launch(w.own.rtiles * w.own.groups * w.own.splits + w.shared.rtiles * w.shared.groups * w.shared.splits) ||
-      !fits_launch((own.out_rows * d / 4 + 255) / 256))
-    return MEA_ERR_INVALID_ARG;
   const int64_t parts = w.shared.splits + w.own.splits;
+  if (!fits_launch(w.own.rtiles * w.own.groups * w.own.splits + w.shared.rtiles * w.shared.groups * w.shared.splits) ||
+      !fits_launch(mea::combine_blocks(own.out_rows, d, parts)))
+    return MEA_ERR_INVALID_ARG;
   carve_parts(&own, p, parts, align256(workspace, 0));
   own.split0 = (int)w.shared.splits;
   StreamParams pre = stream_params(p, score_args(p, nullptr), kv, w.shared);

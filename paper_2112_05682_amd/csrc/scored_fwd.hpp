@@ -516,24 +516,40 @@ __global__ __launch_bounds__(256, (StreamTile<T, D, RWA>::OCC)) void scored_pair
 }
 
 // Combine of the summaries of n_parts key ranges (Section 4): rescaled to the
-// common maximum, added, divided.  A thread per row and 4 features.
-template <typename T, int D>
+// common maximum, added, divided.  A thread per row and 4 features; with SHARES > 1 the
+// threads of a row take a share of the ranges each (of few rows and many ranges, a
+// chain of loads is all it takes), whose sums meet in LDS, in order.
+template <typename T, int D, int SHARES>
 __global__ __launch_bounds__(256) void scored_combine_kernel(StreamParams p, int n_parts) {
-  constexpr int G4 = D / 4;
-  const int64_t gid = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (gid >= p.out_rows * G4) return;
-  const int64_t row = gid / G4;
+  constexpr int G4 = D / 4, NT = 256 / SHARES, N = SHARES > 1 ? 4 : 8;
+  const int share = threadIdx.x / NT, t = threadIdx.x % NT;
+  const int64_t gid = (int64_t)blockIdx.x * NT + t;
+  const bool in_rows = gid < p.out_rows * G4;
+  const int64_t row = in_rows ? gid / G4 : 0;
   const int f0 = 4 * (int)(gid % G4);
   float m = -INFINITY, l = 0.0f;
   f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
-  // Eight ranges at a time, their loads in flight together.
-  for (int s0 = 0; s0 < n_parts; s0 += 8) {
-    float ms[8], ls[8];
-    f32x4 os[8];
+  auto add = [&](float mi, float li, f32x4 oi, float mx) {
+    // (0 times a NaN denominator, a range of NaN scores only, stays NaN)
+    const float w = mi == -INFINITY ? 0.0f : fast_exp2(mi - mx);
+    l = fmaf(w, li, l);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const bool in = s0 + i < n_parts;
-      const int64_t at = (int64_t)(in ? s0 + i : s0) * p.out_rows + row;
+    for (int e = 0; e < 4; ++e) o[e] = fmaf(w, oi[e], o[e]);
+  };
+  auto rescale = [&](float mx) {
+    const float a = m == -INFINITY ? 0.0f : fast_exp2(m - mx);
+    l *= a;
+    o *= a;
+    m = mx;
+  };
+  // N ranges at a time, their loads in flight together.
+  for (int s0 = share; s0 < n_parts; s0 += N * SHARES) {
+    float ms[N], ls[N];
+    f32x4 os[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const bool in = s0 + i * SHARES < n_parts;
+      const int64_t at = (int64_t)(in ? s0 + i * SHARES : s0) * p.out_rows + row;
       ms[i] = p.part_m[at];
       ls[i] = p.part_l[at];
       os[i] = *reinterpret_cast<const f32x4*>(p.part_o + at * D + f0);
@@ -541,20 +557,27 @@ __global__ __launch_bounds__(256) void scored_combine_kernel(StreamParams p, int
     }
     float mx = m;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) mx = fmaxf(mx, ms[i]);
-    const float a = m == -INFINITY ? 0.0f : fast_exp2(m - mx);
-    l *= a;
-    o *= a;
+    for (int i = 0; i < N; ++i) mx = fmaxf(mx, ms[i]);
+    rescale(mx);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      // (0 times a NaN denominator, a range of NaN scores only, stays NaN)
-      const float w = ms[i] == -INFINITY ? 0.0f : fast_exp2(ms[i] - mx);
-      l = fmaf(w, ls[i], l);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) o[e] = fmaf(w, os[i][e], o[e]);
-    }
-    m = mx;
+    for (int i = 0; i < N; ++i) add(ms[i], ls[i], os[i], mx);
   }
+  if constexpr (SHARES > 1) {
+    __shared__ __align__(16) f32x4 os[SHARES][NT];
+    __shared__ float ms[SHARES][NT], ls[SHARES][NT];
+    os[share][t] = o;
+    ms[share][t] = m;
+    ls[share][t] = l;
+    __syncthreads();
+    if (share) return;
+    float mx = m;
+#pragma unroll
+    for (int i = 1; i < SHARES; ++i) mx = fmaxf(mx, ms[i][t]);
+    rescale(mx);
+#pragma unroll
+    for (int i = 1; i < SHARES; ++i) add(ms[i][t], ls[i][t], os[i][t], mx);
+  }
+  if (!in_rows) return;
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;
   float x4[4];
 #pragma unroll
@@ -637,10 +660,14 @@ template <typename T>
 hipError_t launch_scored_combine(const StreamParams& p, int d, int n_parts, hipStream_t stream) {
   StreamParams q = p;
   void* args[] = {&q, &n_parts};
-  const int64_t threads = p.out_rows * (d / 4);
-  const void* k = d == 64 ? reinterpret_cast<const void*>(scored_combine_kernel<T, 64>)
-                          : reinterpret_cast<const void*>(scored_combine_kernel<T, 128>);
-  return hipLaunchKernel(k, dim3((unsigned)((threads + 255) / 256)), dim3(256), args, 0, stream);
+  const void* k;
+  if (combine_shares(n_parts) > 1)
+    k = d == 64 ? reinterpret_cast<const void*>(scored_combine_kernel<T, 64, kCombineShares>)
+                : reinterpret_cast<const void*>(scored_combine_kernel<T, 128, kCombineShares>);
+  else
+    k = d == 64 ? reinterpret_cast<const void*>(scored_combine_kernel<T, 64, 1>)
+                : reinterpret_cast<const void*>(scored_combine_kernel<T, 128, 1>);
+  return hipLaunchKernel(k, dim3((unsigned)combine_blocks(p.out_rows, d, n_parts)), dim3(256), args, 0, stream);
 }
 
 }  // namespace mea

@@ -274,3 +274,24 @@ def test_offsets_beyond_32_bits(n_q):
         pre = attention_shared_prefix(qq, long[0], long[0], tail[None, None].contiguous(), tail[None, None].contiguous())
         want = (2 * s / (2 * s.sum(1, keepdim=True) + rows - 3)) @ tail.double()
         assert ((pre[0, :, 0].double() - want).abs() <= 2.0 ** -7 * 2 * size + 1e-12).all()
+
+
+@pytest.mark.parametrize("dtype,d,n_q", [(torch.bfloat16, 64, 1), (torch.float16, 128, 3), (torch.float32, 64, 2)])
+def test_many_ranges(dtype, d, n_q):
+    """Few rows on a long cache: ranges up to the most there are, the short sequence's mostly
+    empty and the empty one's all; the same against a shared prefix of that length."""
+    B, H, n_k = 3, 4, 40000
+    q, k, v = randn(B, H, n_q, d, dtype=dtype, seed=1, std=3.0), *(randn(B, 1, n_k, d, dtype=dtype, seed=s) for s in (2, 3))
+    lens = [n_k, 700, 0]
+    want = reference(*(t.cpu() for t in (q, k, v)), dtype=dtype, kv_len=lens)
+    for b, n in enumerate(lens):
+        k[b, :, n:], v[b, :, n:] = float("nan"), float("nan")
+    o, lse, o_lo = attention_scored_fwd(q, k, v, kv_len=int32(*lens), residual=True)
+    assert_within("o", o, want["o"])
+    assert_within("lse", lse, want["lse"])
+    for b, n in enumerate(lens[:2]):
+        one = [t[b:b + 1, :, :n] for t in (k, v)]
+        want = reference(q[b:b + 1].cpu(), *(t.cpu() for t in one), dtype=dtype)
+        o, lse = attention_shared_prefix(q[b:b + 1], *(t[0, :, 5:] for t in one), *(t[:, :, :5] for t in one), need_lse=True)
+        assert_within("o", o, want["o"])
+        assert_within("lse", lse, want["lse"])
