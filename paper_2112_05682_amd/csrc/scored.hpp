@@ -185,10 +185,13 @@ __device__ __forceinline__ float table_value(const ScoreArgs& s, int bucket, int
   else x = (float)static_cast<const __bf16*>(s.table)[at];
   return x * per_unit;
 }
-// Bucket of a side for a distance >= 0: the last one that starts at most there.
-__device__ __forceinline__ int side_bucket(const ScoreArgs& s, int distance) {
+// The edges across a wave's lanes, and the bucket of a side for a distance >= 0 (the
+// last one that starts at most there).  All lanes have to be active: edges are read
+// from other lanes' registers, as a chain of scalar loads took 2 us a workgroup.
+__device__ __forceinline__ int lane_edge(const ScoreArgs& s, int lane) { return s.edges[lane < s.n_edges ? lane : 0]; }
+__device__ __forceinline__ int side_bucket(const ScoreArgs& s, int edge, int distance) {
   int n = 0;
-  for (int e = 0; e < s.n_edges; ++e) n += s.edges[e] <= distance;
+  for (int e = 0; e < s.n_edges; ++e) n += __builtin_amdgcn_readlane(edge, e) <= distance;
   return n - 1;
 }
 // The bias by place: place x stands for the distance j - pos = x - span - kPad.  Where
@@ -200,10 +203,10 @@ __host__ __device__ __forceinline__ int bias_ahead(const ScoreArgs& s) { return 
 __host__ __device__ __forceinline__ int bias_places(const ScoreArgs& s) {
   return s.table ? s.span + bias_ahead(s) + 1 + 2 * kPad : 0;
 }
-__device__ __forceinline__ int place_bucket(const ScoreArgs& s, int x) {
+__device__ __forceinline__ int place_bucket(const ScoreArgs& s, int edge, int x) {
   int d = x - s.span - kPad;
   if (d > bias_ahead(s)) d = bias_ahead(s);
-  return side_bucket(s, d < 0 ? -d : d) + (d > 0 ? s.n_edges : 0);
+  return side_bucket(s, edge, d < 0 ? -d : d) + (d > 0 ? s.n_edges : 0);
 }
 // LDS bytes of the bias for fold heads: the values by place, or (several heads)
 // each place's bucket and the heads' buckets.
@@ -214,14 +217,15 @@ __host__ __device__ __forceinline__ int bias_lds_bytes(const ScoreArgs& s, int f
   return (n + 15) / 16 * 16 + (4 * fold * s.n_edges * (s.two_sided ? 2 : 1) + 15) / 16 * 16;
 }
 __device__ __forceinline__ void fill_bias(const ScoreArgs& s, unsigned char* lds, int fold, int head0, int tid, int nt) {
-  const int n = bias_places(s);
+  const int n = bias_places(s), edge = lane_edge(s, tid & 63);
   const float per_unit = kLog2eF / s.unit;
-  if (fold == 1) {
-    for (int x = tid; x < n; x += nt)
-      reinterpret_cast<float*>(lds)[x] = table_value(s, place_bucket(s, x), head0, per_unit);
-    return;
+  for (int x0 = 0; x0 < n; x0 += nt) {
+    const int x = x0 + tid, bucket = place_bucket(s, edge, x);
+    if (x >= n) continue;
+    if (fold == 1) reinterpret_cast<float*>(lds)[x] = table_value(s, bucket, head0, per_unit);
+    else lds[x] = (unsigned char)bucket;
   }
-  for (int x = tid; x < n; x += nt) lds[x] = (unsigned char)place_bucket(s, x);
+  if (fold == 1) return;
   const int nb = s.n_edges * (s.two_sided ? 2 : 1);
   float* tab = reinterpret_cast<float*>(lds + (n + 15) / 16 * 16);
   for (int e = tid; e < fold * nb; e += nt) tab[e] = table_value(s, e % nb, head0 + e / nb, per_unit);

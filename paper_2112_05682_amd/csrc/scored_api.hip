@@ -419,7 +419,8 @@ mea_status mea_scored_attention_bwd(const mea_problem* p, const mea_score* s, co
     a.s.k_range = rk;
     at += (w.ranges_q + w.ranges_k) / 4;
     hipError_t e = mea::launch_doc_ranges(s->q_doc, p->n_q, p->batch, rq, stream);
-    if (e == hipSuccess) e = mea::launch_doc_ranges(s->k_doc, p->n_k, p->batch, rk, stream);
+    if (s->q_doc == s->k_doc && p->n_q == p->n_k) a.s.k_range = rq;
+    else if (e == hipSuccess) e = mea::launch_doc_ranges(s->k_doc, p->n_k, p->batch, rk, stream);
     if (e != hipSuccess) return MEA_ERR_HIP;
   }
   if (d_table) a.table_part = at;

@@ -634,7 +634,7 @@ __device__ __forceinline__ void dq_workgroup(const ScoredBwdParams& p, int block
   if (BIAS && sa.table) {
     fill_bias(sa, lds_bias, 1, head, tid, C::NT);
     if (sums)
-      for (int x = tid; x < 4 * places + 8192; x += C::NT) bins[x] = 0.0f;
+      for (int x = tid; x < places + 2048; x += C::NT) reinterpret_cast<f32x4*>(bins)[x] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   }
 
   Frag<T> qf[KC], gf[KC];
@@ -884,9 +884,11 @@ __device__ __forceinline__ void dq_workgroup(const ScoredBwdParams& p, int block
     const int nb = sa.n_edges * (sa.two_sided ? 2 : 1), zero = sa.span + kPad;  // place of distance 0
     // Workgroups of one head are neighbours in table_part: [head][batch][query tile][part].
     float* const to = p.table_part + ((((int64_t)head * p.n_b + b) * p.n_qtiles + qtile) * p.dq_parts + part) * nb;
-    for (int e = tid; e < nb; e += C::NT) {
+    // 8 lanes a bucket: a chain of reads by one took 3 us where a bucket has 100 places.
+    for (int e0 = 0; e0 < nb; e0 += C::NT / 8) {
+      const int e = e0 + tid / 8;
       const bool ahead = e >= sa.n_edges;
-      const int s = ahead ? e - sa.n_edges : e;
+      const int s = e >= nb ? 0 : (ahead ? e - sa.n_edges : e);
       // Its places [lo, end).
       int lo = s + 1 < sa.n_edges ? sa.edges[s] : sa.span, end = s + 1 < sa.n_edges ? sa.edges[s + 1] : sa.span + 1 + kPad;
       if (ahead) {
@@ -897,9 +899,12 @@ __device__ __forceinline__ void dq_workgroup(const ScoredBwdParams& p, int block
         end = s == 0 && !sa.two_sided ? places : zero - lo + 1;
         lo = from;
       }
+      if (e >= nb) end = lo;
       float y = 0.0f;
-      for (int x = lo; x < end; ++x) y += bins[x];
-      to[e] = y;
+      for (int x = lo + (tid & 7); x < end; x += 8) y += bins[x];
+#pragma unroll
+      for (int o = 4; o > 0; o >>= 1) y += __shfl_xor(y, o);
+      if (e < nb && (tid & 7) == 0) to[e] = y;
     }
   }
 }
