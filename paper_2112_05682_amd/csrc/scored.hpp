@@ -255,9 +255,8 @@ __device__ __forceinline__ float cap_tanh(const ScoreArgs& s, float x) {
   return t;
 }
 
-// A value that the compiler takes as made here, so that what depends on it stays in
-// this branch: as selects on the branch's condition, the masks of a few tiles cost every
-// tile two instructions an element (an empty volatile statement did not prevent it).
+// A value that the compiler takes as made here: what depends on it is not computed
+// ahead of the branch that it stands in (masks of a few tiles, in every tile's code).
 __device__ __forceinline__ void stay(int& x) { asm volatile("" : "+v"(x)); }
 __device__ __forceinline__ void stay(float& x) { asm volatile("" : "+v"(x)); }
 
