@@ -225,6 +225,9 @@ mea_status mea_attention_bwd_noalloc(const mea_problem* p, const void* q, const 
  * (two_sided = 0): the distance is max(pos_i - j, 0).  Two-sided: |j - pos_i|,
  * and keys ahead (j > pos_i) take buckets n_edges .. 2 n_edges - 1.
  *
+ * A table value of -inf hides the pairs of its bucket; a value counts as
+ * infinite if its quotient by scale (with softcap, by softcap) passes float32.
+ *
  * The mea_problem's own mask, padding, strides, dtype and scale hold as before
  * (strides of k, v, dk and dv are over kv_heads); out_f32 must be 0 and d_v must
  * be d.  Everything said above about pointers, streams, workspaces, errors and

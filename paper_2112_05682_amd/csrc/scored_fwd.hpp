@@ -325,8 +325,8 @@ __device__ __forceinline__ void stream_workgroup(const StreamParams& p, int bloc
         for (int r = 0; r < 16; ++r) acc[dt][r] *= alpha;
       m_ref = m_new;
     }
-    // A row with no visible key so far: its (all -inf) exponents get weight 0.
-    const float neg = m_ref == -INFINITY ? 0.0f : fmaf(add, unit, -m_ref);
+    // A row with no visible key so far: its exponents (all -inf, or add is) get weight 0.
+    const float neg = m_ref == -INFINITY ? add : fmaf(add, unit, -m_ref);
     auto weight = [&](int pc, int e) __attribute__((always_inline)) {
       return fast_exp2(fmaf(s[pc >> 1][8 * (pc & 1) + e], unit, neg));
     };

@@ -20,6 +20,7 @@
 #include <ATen/ops/empty.h>
 #include <ATen/ops/empty_like.h>
 #include <c10/core/DeviceGuard.h>
+#include <c10/hip/HIPGraphsC10Utils.h>
 #include <c10/hip/HIPStream.h>
 
 #include <cmath>
@@ -674,10 +675,31 @@ struct ScoredNode : public torch::autograd::Function<ScoredNode> {
   }
 };
 
+// Whether the current stream is being captured into a graph while t is a leaf of a
+// graph recorded on another stream that still lives: autograd would run the leaf's end of
+// the captured backward on that stream, which ends the capture and often the process.
+bool leaf_of_other_stream(const at::Tensor& t) {
+  if (!t.requires_grad() || !t.is_leaf()) return false;
+  const auto end = torch::autograd::impl::try_get_grad_accumulator(t);
+  if (!end) return false;
+  const auto stream = end->stream();
+  return stream && *stream != c10::hip::getCurrentHIPStream(t.device().index()).unwrap();
+}
+
 // scored_apply(q, k, v, causal, scale, kv_len, <score>): o, with its gradient, or None.
 PyObject* ext_scored_apply(PyObject*, PyObject* const* a, Py_ssize_t n) {
   HANDLE_TH_ERRORS
   if (n != 14) return none();
+  if (at::GradMode::is_enabled() && c10::hip::currentStreamCaptureStatusMayInitCtx() != c10::hip::CaptureStatus::None)
+    for (PyObject* o : {a[0], a[1], a[2], a[8]}) {
+      const at::Tensor* t = gpu_tensor(o);
+      if (t && leaf_of_other_stream(*t)) {
+        PyErr_SetString(PyExc_RuntimeError,
+                        "attention_scored: a leaf of this captured call belongs to a graph recorded on another stream that "
+                        "still lives; free that graph's outputs before the capture, or record it on the capture's stream");
+        return nullptr;
+      }
+    }
   const at::Tensor *q = gpu_tensor(a[0]), *k = gpu_tensor(a[1]), *v = gpu_tensor(a[2]), *bias;
   if (!q || !k || !v) return none();
   const at::ScalarType dt = q->scalar_type();

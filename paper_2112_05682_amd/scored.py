@@ -173,7 +173,7 @@ def attention_scored_fwd(q, k, v, causal: bool = False, scale: float | None = No
     ``softcap``: a positive number.  ``slopes``: float32 ``[H]`` on the GPU, no gradient.  ``bias``:
     ``[buckets, H]`` (float32 or q's dtype), whose bucket of a distance is that of ``bucket_edges``;
     ``bidirectional`` (default: not ``causal``) gives each direction half the buckets, else keys
-    ahead count as distance 0.  ``docs``: int32 ``[B, n]`` document of every token, negative for
+    ahead count as distance 0; a value of -inf hides its pairs.  ``docs``: int32 ``[B, n]`` document of every token, negative for
     none, or a pair of those of the queries and of the keys.  ``prefix_len``, ``q_pos`` (position of
     the first query; 0 without it, negative values read as 0) and ``kv_len``: int32 ``[B]``.  For a
     step of decoding against a cache, ``q_pos = kv_len - n_q``."""
@@ -274,7 +274,8 @@ def attention_scored(q, k, v, causal: bool = False, scale: float | None = None, 
                      slopes=None, bias=None, max_distance: int = 128, bidirectional: bool | None = None, docs=None,
                      prefix_len=None, q_pos=None):
     """Attention with modified scores, differentiable in q, k, v and bias, O(n) extra memory;
-    the arguments are those of ``attention_scored_fwd``."""
+    the arguments are those of ``attention_scored_fwd``.  Captured into a graph with its gradient,
+    it is refused while a graph of the same leaves that was recorded on another stream lives."""
     if slopes is not None and slopes.requires_grad:
         raise ValueError("slopes get no gradient: pass them detached")
     docs = tuple(docs) if isinstance(docs, list) else docs

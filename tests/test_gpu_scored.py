@@ -238,3 +238,36 @@ def test_parts_of_the_gradient():
         part = attention_scored_bwd(q, k, v, o, lse, do, need_dq=need[0], need_dkdv=need[1], need_dbias=need[2], o_lo=o_lo, **m)
         for x, y, n in zip(part, full, (need[0], need[1], need[1], need[2])):
             assert (torch.equal(x, y) if n else x is None)
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 64), ("bf16", 128), ("fp32", 64)])
+def test_a_bias_of_minus_infinity_hides(dtype, d):
+    """A window: far keys' bucket is -inf, also of the first tiles that a row meets.  The same
+    bits as with -10^4, whose weights are 0 (2^-14000 of the nearest key's)."""
+    B, H, Hkv, n = 2, 4, 2, 700
+    q, k, v, do = inputs(dtype, B, H, Hkv, n, n, d, seed=3)
+    t = table(32, H, DT[dtype])
+    t[31] = -1e4
+    hidden = t.clone()
+    hidden[31] = float("-inf")
+    ref = reference(q, k, v, do, dtype=DT[dtype], causal=True, bias=t, max_distance=40)
+    dev = [x.cuda() for x in (q, k, v)]
+    got = []
+    for bias in (t.cuda(), hidden.cuda()):
+        kw = dict(causal=True, bias=bias, max_distance=40)
+        o, lse, o_lo = attention_scored_fwd(*dev, residual=True, **kw)
+        grads = attention_scored_bwd(*dev, o, lse, do.cuda(), o_lo=o_lo, **kw)
+        last = attention_scored_fwd(dev[0][:, :, -2:], *dev[1:], q_pos=torch.full((B,), n - 2, dtype=torch.int32, device="cuda"),
+                                    **kw)
+        got.append((o, lse, *grads, *last))
+    torch.cuda.synchronize()
+    for name, x in zip(("o", "lse", "dq", "dk", "dv", "dbias"), got[0]):
+        assert_within(name, x, ref[name])
+    for a, b in zip(*got):
+        assert torch.equal(a, b)
+    # Every bucket: rows that see nothing.
+    kw = dict(causal=True, bias=torch.full_like(t, float("-inf")).cuda(), max_distance=40)
+    o, lse, o_lo = attention_scored_fwd(*dev, residual=True, **kw)
+    for x in (o, *attention_scored_bwd(*dev, o, lse, do.cuda(), o_lo=o_lo, **kw)):
+        assert not x.any()
+    assert (lse == float("-inf")).all()

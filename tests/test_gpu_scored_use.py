@@ -295,3 +295,41 @@ def test_many_ranges(dtype, d, n_q):
         o, lse = attention_shared_prefix(q[b:b + 1], *(t[0, :, 5:] for t in one), *(t[:, :, :5] for t in one), need_lse=True)
         assert_within("o", o, want["o"])
         assert_within("lse", lse, want["lse"])
+
+
+def test_a_captured_gradient_beside_an_eager_graph():
+    """Refused while an eager graph of the same leaves lives (before anything is recorded);
+    captured and replayed once it is gone."""
+    B, H, n, d = 2, 4, 130, 64
+    leaves = [randn(B, H, n, d, seed=i).requires_grad_() for i in range(3)] + [randn(16, H, seed=4).requires_grad_()]
+    do, buf = randn(B, H, n, d, seed=5), torch.ones(4, device="cuda")
+
+    def step():
+        o = attention_scored(*leaves[:3], causal=True, bias=leaves[3], max_distance=50)
+        return (o.detach(), *torch.autograd.grad(o, leaves, do))
+
+    alive = attention_scored(*leaves[:3], causal=True, bias=leaves[3], max_distance=50)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        buf.zero_()
+        with pytest.raises(RuntimeError, match="still lives"):
+            step()
+    del alive, graph
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured = step()
+    for i in range(4):
+        with torch.no_grad():
+            for j, t in enumerate(leaves):
+                t.copy_(randn(*t.shape, seed=100 + 10 * i + j))
+        eager = step()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(captured, eager):
+            assert torch.equal(a, b)
