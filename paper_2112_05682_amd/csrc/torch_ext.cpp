@@ -690,6 +690,8 @@ bool leaf_of_other_stream(const at::Tensor& t) {
 PyObject* ext_scored_apply(PyObject*, PyObject* const* a, Py_ssize_t n) {
   HANDLE_TH_ERRORS
   if (n != 14) return none();
+  const at::Tensor *q = gpu_tensor(a[0]), *k = gpu_tensor(a[1]), *v = gpu_tensor(a[2]), *bias;
+  if (!q || !k || !v) return none();
   if (at::GradMode::is_enabled() && c10::hip::currentStreamCaptureStatusMayInitCtx() != c10::hip::CaptureStatus::None)
     for (PyObject* o : {a[0], a[1], a[2], a[8]}) {
       const at::Tensor* t = gpu_tensor(o);
@@ -700,8 +702,6 @@ PyObject* ext_scored_apply(PyObject*, PyObject* const* a, Py_ssize_t n) {
         return nullptr;
       }
     }
-  const at::Tensor *q = gpu_tensor(a[0]), *k = gpu_tensor(a[1]), *v = gpu_tensor(a[2]), *bias;
-  if (!q || !k || !v) return none();
   const at::ScalarType dt = q->scalar_type();
   if (dtype_code(dt) < 0 || !in_place(*q) || !like(*k, *q, dt) || !like(*v, *q, dt) || !grouped_shapes(*q, *k, *v))
     return none();
