@@ -94,19 +94,25 @@ struct StreamPlan {
 
 // Workgroups of these row waves that the chip holds at once.
 int64_t places_of(const mea_problem* p, int row_waves) {
-  if (p->dtype == MEA_F32) return 256;
+  if (p->dtype == MEA_F32) return row_waves == 4 && p->d == 64 ? 512 : 256;
   return 256 * (row_waves == 1 && p->d == 128 ? 1 : 2);
 }
 // Row tiles, and key ranges for the places that `taken` workgroups leave.  At most 256
 // ranges; us at 64 / 128 / 256 of them, one token, 8 heads of one key head: bf16 d = 128
 // 131072 keys 30 / 23 / 22, d = 64 65536 keys 18 / 15 / 15, float32 65536 keys 85 / 50 / 36.
-void set_tiles(StreamPlan* pl, const mea_problem* p, int rw, int64_t n_keys, int64_t taken) {
+// A range has two tiles and more; of float32, whose tiles take longer than the combine
+// (about 2 us each), one of 64 keys or four of 32: us in 1 / 2 / 3 / 4 / 6 ranges, causal
+// d = 64, 4 heads, 300 (5 tiles of 64) 19 / 17 / 15 / 15 / 13, 2x8 heads, 700 (22 of 32) 48 / 34 /
+// 29 / 27 / 28.  fill: workgroups wanted for each place.
+void set_tiles(StreamPlan* pl, const mea_problem* p, int rw, int64_t n_keys, int64_t taken, double fill = 1.0) {
   pl->row_waves = rw;
   pl->rtiles = (pl->rows + 32 * rw - 1) / (32 * rw);
-  const int64_t wgs = pl->groups * pl->rtiles, tile = mea::stream_tile(p->dtype != MEA_F32, rw);
-  const int64_t key_tiles = (n_keys + tile - 1) / tile, places = places_of(p, rw);
+  const bool is16 = p->dtype != MEA_F32;
+  const int64_t wgs = pl->groups * pl->rtiles, tile = mea::stream_tile(is16, rw);
+  const int64_t key_tiles = (n_keys + tile - 1) / tile, places = (int64_t)(fill * (double)places_of(p, rw));
+  const int64_t most = is16 ? key_tiles / 2 : (rw == 4 ? key_tiles / 4 : (key_tiles > 2 ? key_tiles : 1));
   int64_t splits = (places - (taken < places / 2 ? taken : places / 2)) / wgs;
-  if (splits > key_tiles / 2) splits = key_tiles / 2;
+  if (splits > most) splits = most;
   if (splits > 256) splits = 256;
   pl->splits = splits < 1 ? 1 : splits;
 }
@@ -131,7 +137,9 @@ StreamPlan plan_stream(const mea_problem* p, const ScoreArgs& s, int64_t kv_head
   if (pl.rows <= 32) rw = 1;
   else if (pl.rows <= 64 && rw > 2) rw = 2;
   if (!is16) rw = pl.rows <= 64 || tiles128 <= 32 ? 2 : 4;
-  set_tiles(&pl, p, rw, p->n_k, 0);
+  // Causal float32 row tiles differ in length: us at 1 / 1.25 of the places, d = 64 16 heads, 1500
+  // 63 / 51; d = 128 12 heads on 4, 900 65 / 52.
+  set_tiles(&pl, p, rw, p->n_k, 0, !is16 && p->causal && p->n_q > 128 ? 1.25 : 1.0);
   return pl;
 }
 
