@@ -117,12 +117,34 @@ void set_tiles(StreamPlan* pl, const mea_problem* p, int rw, int64_t n_keys, int
   pl->splits = splits < 1 ? 1 : splits;
 }
 
+// What a 16-bit stream kernel with many row tiles takes: us to start and end, us per
+// 1000 keys of the workgroups of a CU (of the fullest without the causal mask, of the
+// average with it) and of the longest workgroup, and, of several ranges, us of the
+// combine and per million numbers of the parts.  Fitted to 68 shapes of 1-64 heads and
+// 512-16384 tokens, d = 64 and 128, in up to 4 ranges (errors 5-10 %); what it chooses
+// takes 1.02 times the best of those measured on average and 1.18 at most, where fixed
+// numbers of row tiles (128 and 256) for 1, 2 and 4 row waves took 1.17 and 2.1 times.
+struct StreamRate {
+  double fixed, load[2], longest[2], combine, part;  // [with the causal mask]
+};
+StreamRate stream_rate(int64_t d, int row_waves) {
+  if (d == 64)
+    return row_waves == 1   ? StreamRate{11.5, {3.81, 4.33}, {0, 0}, 0, 0}
+           : row_waves == 2 ? StreamRate{8.2, {4.86, 3.19}, {3.27, 7.14}, 3.7, 1.72}
+                            : StreamRate{7.7, {7.34, 4.40}, {5.85, 11.4}, 3.6, 1.38};
+  return row_waves == 1   ? StreamRate{19.5, {8.22, 9.97}, {0, 0}, 0, 0}
+         : row_waves == 2 ? StreamRate{10.5, {9.72, 7.65}, {0, 6.63}, 2.1, 1.87}
+                          : StreamRate{10.4, {14.2, 9.53}, {3.94, 13.6}, 0.5, 1.51};
+}
+
 // Fold: with few queries (a 32-row tile of one head would be padding) the heads that share a key head are rows of the same
 // tile, so that the keys are read once for all of them; with many, each head has
 // tiles of its own (the keys are then found in L2).  Row waves: as few as hold
 // the rows, and on small grids fewer still, so that the waves without rows of
 // their own take shares of the keys instead.  Splits: enough key ranges for about
-// one workgroup for each place on the chip, of at least two tiles each.
+// one workgroup for each place on the chip, of at least two tiles each.  More than 128
+// row tiles of 16 bits: what stream_rate says is fastest, in ranges of 256 keys and more
+// (documents, of whose keys a row tile sees a part: one range).
 StreamPlan plan_stream(const mea_problem* p, const ScoreArgs& s, int64_t kv_heads) {
   StreamPlan pl;
   const bool is16 = p->dtype != MEA_F32;
@@ -133,6 +155,30 @@ StreamPlan plan_stream(const mea_problem* p, const ScoreArgs& s, int64_t kv_head
   pl.rows = p->n_q * pl.fold;
   pl.groups = p->heads / pl.fold * p->batch;
   const int64_t tiles128 = pl.groups * ((pl.rows + 127) / 128);
+  if (is16 && tiles128 > 128 && pl.rows > 64 && !s.q_doc) {
+    const int64_t longest = p->causal && !s.q_pos && p->n_q < p->n_k ? p->n_q : p->n_k;
+    const double mean = (double)longest - (p->causal ? 0.5 * (double)(p->n_q < longest ? p->n_q : longest) : 0.0);
+    const int masked = mean < 0.75 * (double)longest;
+    double best = 0.0;
+    for (int rw = 1; rw <= 4; rw *= 2) {
+      const StreamRate r = stream_rate(p->d, rw);
+      const int64_t tiles = pl.groups * ((pl.rows + 32 * rw - 1) / (32 * rw));
+      for (int64_t n = 1; n <= 8; n += n < 4 ? 1 : 2) {
+        if (n > 1 && (rw == 1 || longest < 256 * n)) break;
+        const double wgs = masked ? (double)tiles / 256.0 : (double)((tiles * n + 255) / 256) / (double)n;
+        double t = r.fixed + (r.load[masked] * wgs * mean + r.longest[masked] * (double)longest / (double)n) / 1000.0;
+        if (n > 1) t += r.combine + r.part * 1e-6 * (double)(n * pl.groups * pl.rows * p->d);
+        if (rw < 4) t *= 1.1;  // caps and biases cost fewer row waves more: us at 2 / 4, slopes 48x1999 64 / 49
+        if (best == 0.0 || t < best) {
+          best = t;
+          pl.row_waves = rw;
+          pl.rtiles = tiles / pl.groups;
+          pl.splits = n;
+        }
+      }
+    }
+    return pl;
+  }
   int rw = tiles128 <= 128 ? 1 : (tiles128 <= 256 ? 2 : 4);
   if (pl.rows <= 32) rw = 1;
   else if (pl.rows <= 64 && rw > 2) rw = 2;
@@ -140,6 +186,7 @@ StreamPlan plan_stream(const mea_problem* p, const ScoreArgs& s, int64_t kv_head
   // Causal float32 row tiles differ in length: us at 1 / 1.25 of the places, d = 64 16 heads, 1500
   // 63 / 51; d = 128 12 heads on 4, 900 65 / 52.
   set_tiles(&pl, p, rw, p->n_k, 0, !is16 && p->causal && p->n_q > 128 ? 1.25 : 1.0);
+  if (is16 && tiles128 > 128 && s.q_doc) pl.splits = 1;
   return pl;
 }
 
