@@ -142,9 +142,11 @@ StreamRate stream_rate(int64_t d, int row_waves) {
 // tiles of its own (the keys are then found in L2).  Row waves: as few as hold
 // the rows, and on small grids fewer still, so that the waves without rows of
 // their own take shares of the keys instead.  Splits: enough key ranges for about
-// one workgroup for each place on the chip, of at least two tiles each.  More than 128
-// row tiles of 16 bits: what stream_rate says is fastest, in ranges of 256 keys and more
-// (documents, of whose keys a row tile sees a part: one range).
+// one workgroup for each place on the chip, of at least two tiles each.  16 bits, about 128
+// row tiles and more (on long keys, 64): what stream_rate says is fastest, in ranges of 256 keys and
+// more (documents, of whose keys a row tile sees a part: one range).  us, before / with it
+// on 64-128 row tiles: d = 64 2x8192 causal 65 / 42, 1x16384 124 / 60; d = 128 1x8192 72 / 43, 2x4096
+// 40 / 32.
 StreamPlan plan_stream(const mea_problem* p, const ScoreArgs& s, int64_t kv_heads) {
   StreamPlan pl;
   const bool is16 = p->dtype != MEA_F32;
@@ -155,12 +157,13 @@ StreamPlan plan_stream(const mea_problem* p, const ScoreArgs& s, int64_t kv_head
   pl.rows = p->n_q * pl.fold;
   pl.groups = p->heads / pl.fold * p->batch;
   const int64_t tiles128 = pl.groups * ((pl.rows + 127) / 128);
-  if (is16 && tiles128 > 128 && pl.rows > 64 && !s.q_doc) {
-    const int64_t longest = p->causal && !s.q_pos && p->n_q < p->n_k ? p->n_q : p->n_k;
+  const int64_t longest = p->causal && !s.q_pos && p->n_q < p->n_k ? p->n_q : p->n_k;
+  const bool many = tiles128 > (p->d == 64 ? 128 : 127);
+  if (is16 && pl.rows > 64 && !s.q_doc && (many || (tiles128 >= 64 && longest >= (p->d == 64 ? 6000 : 3000)))) {
     const double mean = (double)longest - (p->causal ? 0.5 * (double)(p->n_q < longest ? p->n_q : longest) : 0.0);
     const int masked = mean < 0.75 * (double)longest;
     double best = 0.0;
-    for (int rw = 1; rw <= 4; rw *= 2) {
+    for (int rw = many ? 1 : 2; rw <= 4; rw *= 2) {
       const StreamRate r = stream_rate(p->d, rw);
       const int64_t tiles = pl.groups * ((pl.rows + 32 * rw - 1) / (32 * rw));
       for (int64_t n = 1; n <= 8; n += n < 4 ? 1 : 2) {
@@ -186,7 +189,13 @@ StreamPlan plan_stream(const mea_problem* p, const ScoreArgs& s, int64_t kv_head
   // Causal float32 row tiles differ in length: us at 1 / 1.25 of the places, d = 64 16 heads, 1500
   // 63 / 51; d = 128 12 heads on 4, 900 65 / 52.
   set_tiles(&pl, p, rw, p->n_k, 0, !is16 && p->causal && p->n_q > 128 ? 1.25 : 1.0);
-  if (is16 && tiles128 > 128 && s.q_doc) pl.splits = 1;
+  if (is16 && many && s.q_doc) pl.splits = 1;
+  // Two workgroups on a CU that one fills hardly: us in 1 / 2 ranges, 16x512 10 / 13, 8x1024
+  // 12 / 15, 4x2048 18 / 17, 2x4096 32 / 23.
+  if (is16 && rw == 1 && p->d == 64 && pl.rows > 64) {
+    const int64_t most = p->n_k < 1536 ? 1 : p->n_k / 768;
+    if (pl.splits > most) pl.splits = most;
+  }
   return pl;
 }
 
