@@ -462,7 +462,8 @@ hipError_t launch_scored_table(const ScoredBwdParams& p, hipStream_t stream);
 hipError_t launch_doc_ranges(const int* ids, int64_t n, int64_t batches, int2* out, hipStream_t stream);
 
 // Rows per workgroup: 32 for each of 4 waves, or 2 or 1 (the other waves take
-// shares of the keys).
+// shares of the keys), or 0: at most kFewRows float32 rows (scored_few.hpp).
+constexpr int kFewRows = 8;
 template <typename T> hipError_t launch_stream(const StreamParams& p, int d, int row_waves, hipStream_t stream);
 // Two key sets in one launch: row waves 4 and 4 or 2, or 1 and 1 (float32: 2 and 2).
 template <typename T>

@@ -94,6 +94,7 @@ struct StreamPlan {
 
 // Workgroups of these row waves that the chip holds at once.
 int64_t places_of(const mea_problem* p, int row_waves) {
+  if (p->dtype == MEA_F32 && row_waves == 0) return 1024;
   if (p->dtype == MEA_F32) return row_waves == 4 && p->d == 64 ? 512 : 256;
   return 256 * (row_waves == 1 && p->d == 128 ? 1 : 2);
 }
@@ -106,11 +107,11 @@ int64_t places_of(const mea_problem* p, int row_waves) {
 // 29 / 27 / 28.  fill: workgroups wanted for each place.
 void set_tiles(StreamPlan* pl, const mea_problem* p, int rw, int64_t n_keys, int64_t taken, double fill = 1.0) {
   pl->row_waves = rw;
-  pl->rtiles = (pl->rows + 32 * rw - 1) / (32 * rw);
+  pl->rtiles = rw ? (pl->rows + 32 * rw - 1) / (32 * rw) : 1;
   const bool is16 = p->dtype != MEA_F32;
   const int64_t wgs = pl->groups * pl->rtiles, tile = mea::stream_tile(is16, rw);
   const int64_t key_tiles = (n_keys + tile - 1) / tile, places = (int64_t)(fill * (double)places_of(p, rw));
-  const int64_t most = is16 ? key_tiles / 2 : (rw == 4 ? key_tiles / 4 : (key_tiles > 2 ? key_tiles : 1));
+  const int64_t most = is16 || rw == 0 ? key_tiles / 2 : (rw == 4 ? key_tiles / 4 : (key_tiles > 2 ? key_tiles : 1));
   int64_t splits = (places - (taken < places / 2 ? taken : places / 2)) / wgs;
   if (splits > most) splits = most;
   if (splits > 256) splits = 256;
@@ -185,7 +186,7 @@ StreamPlan plan_stream(const mea_problem* p, const ScoreArgs& s, int64_t kv_head
   int rw = tiles128 <= 128 ? 1 : (tiles128 <= 256 ? 2 : 4);
   if (pl.rows <= 32) rw = 1;
   else if (pl.rows <= 64 && rw > 2) rw = 2;
-  if (!is16) rw = pl.rows <= 64 || tiles128 <= 32 ? 2 : 4;
+  if (!is16) rw = pl.rows <= mea::kFewRows && !s.q_doc ? 0 : (pl.rows <= 64 || tiles128 <= 32 ? 2 : 4);
   // Causal float32 row tiles differ in length: us at 1 / 1.25 of the places, d = 64 16 heads, 1500
   // 63 / 51; d = 128 12 heads on 4, 900 65 / 52.
   set_tiles(&pl, p, rw, p->n_k, 0, !is16 && p->causal && p->n_q > 128 ? 1.25 : 1.0);

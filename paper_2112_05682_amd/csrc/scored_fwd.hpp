@@ -18,6 +18,7 @@
 #pragma once
 
 #include "scored.hpp"
+#include "scored_few.hpp"
 
 namespace mea {
 
@@ -656,6 +657,9 @@ static hipError_t launch_stream_rows(const StreamParams& p, int row_waves, hipSt
     case 2: return launch_stream_mods<T, D, 2>(p, stream);
     case 1:
       if constexpr (sizeof(T) == 2) return launch_stream_mods<T, D, 1>(p, stream);
+      break;
+    case 0:
+      if constexpr (sizeof(T) == 4) return launch_stream_few<D>(p, stream);
   }
   return hipErrorInvalidValue;
 }

@@ -32,7 +32,8 @@ void use(const char* name, const void* p, size_t bytes) {
   if (p) g_spans.push_back({name, (uintptr_t)p, bytes});
 }
 void stream_parts(const mea::StreamParams& p, int d, int rw, bool is16) {
-  expect(rw == 4 || rw == 2 || (rw == 1 && is16), "row waves");
+  expect(rw == 4 || rw == 2 || (rw == 1 && is16) || (rw == 0 && !is16 && p.group_rows <= mea::kFewRows && !p.s.q_doc),
+         "row waves");
   expect(p.fold >= 1 && p.heads_per_kv % p.fold == 0, "fold");
   expect(p.groups_per_kv * p.fold == p.heads_per_kv, "groups of a key head");
   expect(p.n_splits >= 1 && p.n_groups >= 1, "grid");

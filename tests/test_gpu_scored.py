@@ -271,3 +271,25 @@ def test_a_bias_of_minus_infinity_hides(dtype, d):
     for x in (o, *attention_scored_bwd(*dev, o, lse, do.cuda(), o_lo=o_lo, **kw)):
         assert not x.any()
     assert (lse == float("-inf")).all()
+
+
+@pytest.mark.parametrize("mod", ["none", "cap", "slopes", "buckets", "prefix", "empty"])
+@pytest.mark.parametrize("case", [("fp32", 3, 8, 1, 1, 1300, 64, [1300, 65, 1]), ("fp32", 2, 6, 2, 2, 700, 128, [700, 31]),
+                                  ("fp32", 1, 5, 5, 1, 3000, 128, [3000]), ("fp32", 2, 2, 2, 8, 500, 64, [500, 8]),
+                                  ("fp32", 300, 4, 1, 1, 40, 64, None)], ids=lambda c: "-".join(map(str, c[:7])))
+def test_few_float32_rows(case, mod):
+    """1 to 8 rows of a key head, in one range and in several."""
+    test_decode(case[:7] + (case[7] or [1 + i % 40 for i in range(case[1])],), mod)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_few_float32_rows_of_a_strided_cache(d):
+    B, H, Hkv, n = 2, 4, 2, 600
+    q, k, v, _ = (t.cuda() for t in inputs("fp32", B, H, Hkv, 1, n, d))
+    want = attention_scored_fwd(q, k, v, softcap=3.0)
+    rows = [t.transpose(1, 2).contiguous().transpose(1, 2) for t in (k, v)]
+    wide = [torch.cat([t, t], 3)[..., :d] for t in (k, v)]
+    out = torch.full((B, 1, H, d), 7.0, device="cuda").transpose(1, 2)
+    for x in (rows, wide):
+        for a, b in zip(attention_scored_fwd(q, *x, softcap=3.0, out=out), want):
+            assert torch.equal(a, b)
