@@ -293,3 +293,23 @@ def test_few_float32_rows_of_a_strided_cache(d):
     for x in (rows, wide):
         for a, b in zip(attention_scored_fwd(q, *x, softcap=3.0, out=out), want):
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype,B,H,Hkv,n,d,mod", [
+    ("bf16", 1, 8, 4, 3000, 64, "buckets"), ("fp16", 1, 4, 1, 6100, 64, "cap"), ("bf16", 1, 2, 1, 4100, 128, "slopes"),
+    ("bf16", 3, 4, 4, 3000, 64, "prefix"), ("bf16", 2, 8, 8, 2000, 128, "none"), ("fp32", 1, 4, 2, 1700, 64, "buckets"),
+    ("fp32", 2, 6, 6, 900, 128, "prefix")])
+def test_key_ranges_of_many_rows(dtype, B, H, Hkv, n, d, mod):
+    """Long heads whose row tiles are split over keys; the first rows, some in the middle, and
+    the last ones against the reference of those rows."""
+    q, k, v, _ = inputs(dtype, B, H, Hkv, n, n, d, seed=11, gain=2.0)
+    mods = {"kv_len": [n - 333 * b for b in range(B)]}
+    mods.update({"none": {}, "cap": {"softcap": 4.0}, "slopes": {"slopes": alibi(H)}, "prefix": {"prefix_len": [n // 3] * B},
+                 "buckets": {"bias": table(32, H, DT[dtype]), "softcap": 30.0}}[mod])
+    o, lse, _ = attention_scored_fwd(q.cuda(), k.cuda(), v.cuda(), causal=True, residual=True, **to_gpu(mods))
+    torch.cuda.synchronize()
+    for start in (0, n // 2 - 7, n - 40):
+        rows = slice(start, start + 40)
+        ref = reference(q[:, :, rows], k, v, dtype=DT[dtype], causal=True, q_pos=[start] * B, **mods)
+        assert_within("o", o[:, :, rows], ref["o"])
+        assert_within("lse", lse[:, :, rows], ref["lse"])
