@@ -123,7 +123,7 @@ void set_tiles(StreamPlan* pl, const mea_problem* p, int rw, int64_t n_keys, int
 // average with it) and of the longest workgroup, and, of several ranges, us of the
 // combine and per million numbers of the parts.  Fitted to 68 shapes of 1-64 heads and
 // 512-16384 tokens, d = 64 and 128, in up to 4 ranges (errors 5-10 %); what it chooses
-// takes 1.02 times the best of those measured on average and 1.18 at most, where fixed
+// takes 1.01 times the best of those measured on average and 1.19 at most, where fixed
 // numbers of row tiles (128 and 256) for 1, 2 and 4 row waves took 1.17 and 2.1 times.
 struct StreamRate {
   double fixed, load[2], longest[2], combine, part;  // [with the causal mask]
